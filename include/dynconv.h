@@ -80,7 +80,10 @@ typedef DYNCONV_ENUM(dynconv_status_e) {
 typedef DYNCONV_ENUM(dynconv_act_e) {
     DYNCONV_ACT_NONE = 0,
     DYNCONV_ACT_RELU = 1,
-    DYNCONV_ACT_RELU6 = 2
+    DYNCONV_ACT_RELU6 = 2,
+    /* token operators (dynconv_grouped_linear and below) only: */
+    DYNCONV_ACT_SILU = 3, /* v / (1 + exp(-v)) */
+    DYNCONV_ACT_GELU = 4  /* v * (1 + erf(v / sqrt 2)) / 2 */
 } dynconv_act;
 
 /* Shape of a feature map: n images of h x w positions and c channels. */
@@ -466,6 +469,170 @@ dynconv_status dynconv_network_forward_profiled(const void *x, void *y, dynconv_
                                                 const dynconv_layer *layers, int32_t n_layers, int32_t flags,
                                                 uint8_t *masks, int32_t *counts, void *ws, size_t ws_bytes,
                                                 void *stream, void *const *events, int32_t n_events);
+
+/*
+ * Token operators: rows executed with weights chosen among many
+ * --------------------------------------------------------------
+ * The blocks above decide per position whether it runs.  These calls decide
+ * which weights a row runs with: a router picks top_k of E experts per row and
+ * lists the assignments by expert, products grouped by those lists read each
+ * expert's weights for its rows only, and a shared projection takes low-rank
+ * adapters per request beside it.  The conventions at the top of this file
+ * hold (device pointers, host validation, one stream, no allocation, HIP graph
+ * capture).  Rows are dense, channel fastest; fp32, fp16 and bf16 storage with
+ * fp32 accumulation.  Widths (c_in, c_hidden, c_out) are multiples of 8 up to
+ * 65536; data and weight pointers 16-byte aligned, lists 4-byte; row counts
+ * below 2^31.  A call on no rows is valid: it enqueues nothing (the router
+ * still writes its empty lists) and may have NULL row pointers.  Values in
+ * device lists are checked by the kernels: an entry outside its range makes
+ * its row (or assignment) one that is not computed, and nothing is read or
+ * written for it.
+ */
+
+/* Routes of `tokens` rows (host struct, device arrays):
+ *   expert [tokens][top_k]  chosen experts in falling order of their key, -1
+ *                           in the slots without one
+ *   weight [tokens][top_k]  fp32, 0 in the slots without an expert
+ *   rows   [tokens*top_k]   assignments a = token*top_k + slot, grouped by
+ *                           expert, ascending in each group; the entries
+ *                           from starts[experts] on are -1
+ *   starts [experts + 1]    group e is rows[starts[e]] .. rows[starts[e+1] - 1]
+ *   capacity                entries that rows has room for
+ */
+typedef struct {
+    int32_t *expert;
+    float *weight;
+    int32_t *rows;
+    int32_t *starts;
+    int64_t capacity;
+} dynconv_routes;
+
+#define DYNCONV_ROUTE_SIGMOID 1     /* weights by sigmoid instead of softmax */
+#define DYNCONV_ROUTE_RENORMALIZE 2 /* weights of a row's chosen experts sum to `scale` */
+
+/* Workspace bytes of dynconv_route (0 for invalid sizes). */
+size_t dynconv_route_workspace_bytes(int64_t tokens, int32_t experts, int32_t top_k);
+
+/*
+ * Top-k router.  key[t][e] = logits[t][e] + bias[e], one fp32 addition; row t
+ * takes the top_k experts of the largest keys, ties to the lowest e (-0 and +0
+ * tie).  Experts whose key is NaN or -inf are never chosen, and a row whose
+ * mask is 0 chooses none.  With l = the unbiased logits in fp32,
+ *   softmax:               w = exp(l) / sum of exp(l) over every expert of the
+ *                          row that could be chosen; renormalised: over the
+ *                          chosen ones (equal infinite maxima share alike)
+ *   DYNCONV_ROUTE_SIGMOID: w = 1 / (1 + exp(-l)); renormalised: over the
+ *                          chosen ones' sum (0 where that is 0)
+ * and weight = scale * w.  The choice and the lists are exact and
+ * deterministic.
+ *   logits (device) [tokens][experts], dtype dt, aligned to its type
+ *   bias   (device) fp32 [experts], finite, or NULL
+ *   mask   (device) uint8 [tokens] (nonzero = routed) or NULL: all rows
+ *   flags  0 / DYNCONV_ROUTE_SIGMOID / DYNCONV_ROUTE_RENORMALIZE (others: ERR_ARG)
+ *   1 <= experts <= 1024, 1 <= top_k <= min(16, experts)
+ */
+dynconv_status dynconv_route(const void *logits, int64_t tokens, dynconv_dtype dt, int32_t experts, int32_t top_k,
+                             const float *bias, const uint8_t *mask, int32_t flags, float scale,
+                             const dynconv_routes *routes, void *ws, size_t ws_bytes, void *stream);
+
+/* One pointwise product, or one per group: w [c_out][c_in] or
+ * [groups][c_out][c_in] in the storage dtype, b fp32 [c_out] or
+ * [groups][c_out] or NULL, and its activation (device pointers). */
+typedef struct {
+    int32_t c_in, c_out;
+    const void *w;
+    const float *b;
+    int32_t act;
+} dynconv_linear;
+
+/*
+ * Products grouped by weight, groups of any sizes: for every list position p
+ * of group g, starts[g] <= p < starts[g + 1],
+ *   y[dst ? dst[p] : p] = act(W_g x[src ? src[p] / src_div : p] + b_g)
+ * With a router's lists, src = rows and src_div = top_k gather the rows of
+ * each expert, and dst = rows puts results back at their assignments.
+ *   x      (device) [x_rows][c_in];  y (device) [y_rows][c_out], not
+ *          overlapping x; rows that no position names stay as they are
+ *   starts (device) int32 [groups + 1], ascending, groups <= 1024; values are
+ *          taken as if cut to 0 .. rows
+ *   rows   list positions; src and dst (device) int32 [rows] or NULL (then
+ *          x_rows or y_rows must be at least rows); the entries of dst are
+ *          distinct; src_div >= 1, 1 without src
+ */
+dynconv_status dynconv_grouped_linear(const void *x, int64_t x_rows, void *y, int64_t y_rows, dynconv_dtype dt,
+                                      const dynconv_linear *l, int32_t groups, const int32_t *starts, int64_t rows,
+                                      const int32_t *src, int32_t src_div, const int32_t *dst, void *stream);
+
+/*
+ * An expert layer: per expert an expansion, optionally gated, and a
+ * projection (device pointers; weights in the storage dtype, biases fp32 or
+ * NULL):
+ *   h = act(W_expand x + b_expand), or with w_gate
+ *   h = act(W_gate x + b_gate) * (W_expand x + b_expand)
+ *   F_e(x) = W_project h + b_project
+ *   w_expand, w_gate [experts][c_hidden][c_in]; w_project [experts][c_out][c_hidden]
+ * h is rounded to the storage type, F_e(x) stays in fp32 until it is summed.
+ */
+typedef struct {
+    int32_t c_in, c_hidden, c_out, experts;
+    const void *w_expand;
+    const float *b_expand;
+    const void *w_gate;
+    const float *b_gate;
+    const void *w_project;
+    const float *b_project;
+    int32_t act;
+} dynconv_experts;
+
+#define DYNCONV_EXPERTS_RESIDUAL 1 /* add the layer's input (c_in == c_out) */
+
+/* Workspace bytes of dynconv_experts_forward (0 for invalid arguments). */
+size_t dynconv_experts_workspace_bytes(int64_t tokens, const dynconv_experts *e, dynconv_dtype dt, int32_t top_k);
+
+/*
+ * y[t] = (x[t] +) sum over the slots s of row t, in slot order, of
+ *        weight[t][s] * F_{expert[t][s]}(x[t])
+ * for routes that dynconv_route made.  A row without experts gives 0, or x[t].
+ *   x (device) [tokens][c_in], y (device) [tokens][c_out]; y == x runs in
+ *   place (c_in == c_out), any other overlap is DYNCONV_ERR_SHAPE
+ */
+dynconv_status dynconv_experts_forward(const void *x, void *y, int64_t tokens, dynconv_dtype dt,
+                                       const dynconv_experts *e, int32_t top_k, const dynconv_routes *routes,
+                                       int32_t flags, void *ws, size_t ws_bytes, void *stream);
+
+/*
+ * Low-rank adapters (device arrays), one per id:
+ *   down [adapters][max_rank][c_in], up [adapters][c_out][max_rank] in the
+ *   storage dtype, max_rank a multiple of 8 up to 256; ranks int32 [adapters]
+ *   or NULL (all max_rank): rows of down from ranks[i] on are not read, columns
+ *   of up from ranks[i] on do not count but have to be finite; scales fp32
+ *   [adapters] or NULL (1)
+ */
+typedef struct {
+    int32_t adapters, max_rank;
+    const void *down;
+    const void *up;
+    const int32_t *ranks;
+    const float *scales;
+} dynconv_adapters;
+
+/* Workspace bytes of dynconv_adapter_linear (0 for invalid arguments). */
+size_t dynconv_adapter_workspace_bytes(int64_t rows, const dynconv_linear *l, const dynconv_adapters *adapters,
+                                       dynconv_dtype dt);
+
+/*
+ * A projection shared by the rows of many requests, each with its own
+ * adapter: with i = ids[r],
+ *   y[r] = act(W x[r] + b + scales[i] * up_i (down_i x[r]))
+ * and y[r] = act(W x[r] + b) where ids[r] is outside 0 .. adapters - 1.  The
+ * rows may come in any order; those of one request side by side run fastest.
+ * scales[i] * down_i x[r] is rounded to the storage type.
+ *   x (device) [rows][c_in], y (device) [rows][c_out], not overlapping
+ *   ids (device) int32 [rows]
+ */
+dynconv_status dynconv_adapter_linear(const void *x, void *y, int64_t rows, dynconv_dtype dt, const dynconv_linear *l,
+                                      const dynconv_adapters *adapters, const int32_t *ids, void *ws, size_t ws_bytes,
+                                      void *stream);
 
 #ifdef __cplusplus
 }

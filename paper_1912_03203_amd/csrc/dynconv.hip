@@ -17,6 +17,8 @@
 #include "kernels.h"
 #include "shuffle.h"
 #include "dense.h"
+#include "grouped.h"
+#include "route.h"
 
 using namespace dynconv;
 
@@ -1821,3 +1823,5 @@ dynconv_status dynconv_network_forward_profiled(const void *x, void *y, dynconv_
 }
 
 }  // extern "C"
+
+#include "tokens.h"

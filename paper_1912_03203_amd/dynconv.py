@@ -34,7 +34,9 @@ EXPORTED = (
     "dynconv_shuffle_stack_forward_profiled", "dynconv_network_output_shape",
     "dynconv_network_workspace_bytes", "dynconv_network_forward", "dynconv_network_launch_names",
     "dynconv_network_forward_profiled", "dynconv_stack_noalloc_max_workspace_bytes",
-    "dynconv_stack_forward_noalloc",
+    "dynconv_stack_forward_noalloc", "dynconv_route_workspace_bytes", "dynconv_route",
+    "dynconv_grouped_linear", "dynconv_experts_workspace_bytes", "dynconv_experts_forward",
+    "dynconv_adapter_workspace_bytes", "dynconv_adapter_linear",
 )
 
 
@@ -147,6 +149,7 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
                                                      i32, vp, vp, vp, sz, vp, ctypes.POINTER(ctypes.c_void_p),
                                                      i32]
     lib.dynconv_network_forward_profiled.restype = ctypes.c_int
+    _declare_tokens(lib)
     _lib = lib
     return lib
 
@@ -552,3 +555,335 @@ class Network:
         _check(self.lib.dynconv_network_forward_profiled(*self._args(stream), arr, len(events)),
                "dynconv_network_forward_profiled")
         return self.y
+
+
+# ---------------------------------------------------------- token operators
+ACT_SILU, ACT_GELU = 3, 4
+ROUTE_SIGMOID, ROUTE_RENORMALIZE = 1, 2
+EXPERTS_RESIDUAL = 1
+
+
+class RoutesStruct(ctypes.Structure):
+    _fields_ = [("expert", ctypes.c_void_p), ("weight", ctypes.c_void_p), ("rows", ctypes.c_void_p),
+                ("starts", ctypes.c_void_p), ("capacity", ctypes.c_int64)]
+
+
+class LinearStruct(ctypes.Structure):
+    _fields_ = [("c_in", ctypes.c_int32), ("c_out", ctypes.c_int32), ("w", ctypes.c_void_p), ("b", ctypes.c_void_p),
+                ("act", ctypes.c_int32)]
+
+
+class ExpertsStruct(ctypes.Structure):
+    _fields_ = [("c_in", ctypes.c_int32), ("c_hidden", ctypes.c_int32), ("c_out", ctypes.c_int32),
+                ("experts", ctypes.c_int32), ("w_expand", ctypes.c_void_p), ("b_expand", ctypes.c_void_p),
+                ("w_gate", ctypes.c_void_p), ("b_gate", ctypes.c_void_p), ("w_project", ctypes.c_void_p),
+                ("b_project", ctypes.c_void_p), ("act", ctypes.c_int32)]
+
+
+class AdaptersStruct(ctypes.Structure):
+    _fields_ = [("adapters", ctypes.c_int32), ("max_rank", ctypes.c_int32), ("down", ctypes.c_void_p),
+                ("up", ctypes.c_void_p), ("ranks", ctypes.c_void_p), ("scales", ctypes.c_void_p)]
+
+
+def _declare_tokens(lib):
+    vp, sz, i32, i64, ci = ctypes.c_void_p, ctypes.c_size_t, ctypes.c_int32, ctypes.c_int64, ctypes.c_int
+    p = ctypes.POINTER
+    for name, res, args in (
+            ("dynconv_route_workspace_bytes", sz, [i64, i32, i32]),
+            ("dynconv_route", ci, [vp, i64, ci, i32, i32, vp, vp, i32, ctypes.c_float, p(RoutesStruct), vp, sz, vp]),
+            ("dynconv_grouped_linear", ci, [vp, i64, vp, i64, ci, p(LinearStruct), i32, vp, i64, vp, i32, vp, vp]),
+            ("dynconv_experts_workspace_bytes", sz, [i64, p(ExpertsStruct), ci, i32]),
+            ("dynconv_experts_forward", ci, [vp, vp, i64, ci, p(ExpertsStruct), i32, p(RoutesStruct), i32, vp, sz, vp]),
+            ("dynconv_adapter_workspace_bytes", sz, [i64, p(LinearStruct), p(AdaptersStruct), ci]),
+            ("dynconv_adapter_linear", ci, [vp, vp, i64, ci, p(LinearStruct), p(AdaptersStruct), vp, vp, sz, vp])):
+        fn = getattr(lib, name)
+        fn.restype, fn.argtypes = res, args
+
+
+def _need(t, name, dtype, shape, like):
+    """t is a dense tensor of this dtype and shape (None: any size) on like's device."""
+    if not isinstance(t, torch.Tensor):
+        raise DynconvError("%s: a tensor is needed" % name)
+    if t.dtype != dtype:
+        raise DynconvError("%s: dtype %s, not %s" % (name, dtype, t.dtype))
+    if t.dim() != len(shape) or any(w is not None and n != w for n, w in zip(t.shape, shape)):
+        raise DynconvError("%s: shape %s, not %s" % (name, tuple(shape), tuple(t.shape)))
+    if not t.is_contiguous():
+        raise DynconvError("%s: the tensor is not contiguous" % name)
+    if t.device != like.device:
+        raise DynconvError("%s: on %s, not on %s" % (name, t.device, like.device))
+
+
+def _storage(x, name):
+    if not isinstance(x, torch.Tensor) or x.dtype not in _CODE:
+        raise DynconvError("%s: an fp32, fp16 or bf16 tensor is needed" % name)
+
+
+class _Prepared:
+    """A call marshalled once: calling it enqueues it on `stream` (default: the
+    current stream of the tensors' device)."""
+
+    def _prepare(self, device, fn, name, args):
+        self._device, self._fn, self._name, self._cargs = device, fn, name, args
+        self._index = device.index if device.index is not None else torch.cuda.current_device()
+
+    def __call__(self, stream=None):
+        if stream is not None and stream.device.index != self._index:
+            raise DynconvError("%s: the stream is on another device" % self._name)
+        if torch.cuda.current_device() == self._index:
+            return self._enqueue(stream)
+        with torch.cuda.device(self._index):
+            return self._enqueue(stream)
+
+    def _enqueue(self, stream):
+        handle = (stream if stream is not None else torch.cuda.current_stream(self._index)).cuda_stream
+        code = self._fn(*self._cargs, handle)
+        if code != 0:
+            _check(code, self._name)
+        return self._result()
+
+
+def _scratch(nbytes, ws, device, name):
+    if nbytes == 0:
+        raise DynconvError("%s rejected the arguments" % name)
+    if ws is None:
+        return torch.empty(nbytes, dtype=torch.uint8, device=device)
+    if ws.device != device or not ws.is_contiguous():
+        raise DynconvError("ws: a contiguous tensor on %s is needed" % device)
+    return ws
+
+
+def _raw(t):
+    return None if t is None or t.numel() == 0 else t.data_ptr()
+
+
+@dataclass
+class Routes:
+    """A router's result (dynconv_routes): expert [T, k] int32, weight [T, k]
+    fp32, rows [T * k] int32, starts [experts + 1] int32."""
+
+    expert: torch.Tensor
+    weight: torch.Tensor
+    rows: torch.Tensor
+    starts: torch.Tensor
+
+    @classmethod
+    def alloc(cls, tokens: int, experts: int, top_k: int, device="cuda"):
+        def new(shape, dtype):
+            return torch.empty(shape, dtype=dtype, device=device)
+
+        return cls(new((tokens, top_k), torch.int32), new((tokens, top_k), torch.float32),
+                   new((tokens * top_k,), torch.int32), new((experts + 1,), torch.int32))
+
+    def check(self, tokens, experts, top_k, like):
+        _need(self.expert, "expert", torch.int32, (tokens, top_k), like)
+        _need(self.weight, "weight", torch.float32, (tokens, top_k), like)
+        _need(self.rows, "rows", torch.int32, (tokens * top_k,), like)
+        _need(self.starts, "starts", torch.int32, (experts + 1,), like)
+
+    def struct(self) -> RoutesStruct:
+        return RoutesStruct(_raw(self.expert), _raw(self.weight), _raw(self.rows), _raw(self.starts), self.rows.numel())
+
+
+class Router(_Prepared):
+    """A prepared dynconv_route call: logits [T, experts] -> Routes."""
+
+    def __init__(self, logits, top_k, bias=None, mask=None, flags=0, scale=1.0, routes=None, ws=None):
+        lib = load()
+        _storage(logits, "logits")
+        _need(logits, "logits", logits.dtype, (None, None), logits)
+        tokens, experts = logits.shape
+        if bias is not None:
+            _need(bias, "bias", torch.float32, (experts,), logits)
+        if mask is not None:
+            _need(mask, "mask", torch.uint8, (tokens,), logits)
+        nbytes = lib.dynconv_route_workspace_bytes(tokens, experts, top_k)
+        self.ws = _scratch(nbytes, ws, logits.device, "dynconv_route_workspace_bytes")
+        self.routes = Routes.alloc(tokens, experts, top_k, logits.device) if routes is None else routes
+        self.routes.check(tokens, experts, top_k, logits)
+        self.keep = (logits, bias, mask)
+        self.struct = self.routes.struct()
+        self._prepare(logits.device, lib.dynconv_route, "dynconv_route",
+                      (_raw(logits), tokens, dtype_code(logits.dtype), experts, top_k, _raw(bias), _raw(mask),
+                       int(flags), float(scale), ctypes.byref(self.struct), self.ws.data_ptr(),
+                       self.ws.numel() * self.ws.element_size()))
+
+    def _result(self):
+        return self.routes
+
+
+def route(logits, top_k, bias=None, mask=None, flags=0, scale=1.0, stream=None) -> Routes:
+    """One dynconv_route call on new buffers of `stream`."""
+    return _once(Router, stream, logits, top_k, bias, mask, flags, scale)
+
+
+def _once(kind, stream, x, *args, **kw):
+    """A prepared call made, run and dropped: what it allocates belongs to the
+    stream it runs on."""
+    if not isinstance(x, torch.Tensor) or not x.is_cuda:
+        raise DynconvError("a device tensor is needed")
+    with torch.cuda.device(x.device):
+        if stream is None:
+            return kind(x, *args, **kw)()
+        with torch.cuda.stream(stream):
+            return kind(x, *args, **kw)(stream)
+
+
+class GroupedLinear(_Prepared):
+    """A prepared dynconv_grouped_linear call: position p of group g, for
+    starts[g] <= p < starts[g + 1], is y[dst[p]] = act(w[g] x[src[p] // src_div] + b[g])
+    (without src or dst: row p)."""
+
+    def __init__(self, x, y, w, b, starts, src=None, src_div=1, dst=None, act=ACT_NONE):
+        lib = load()
+        _storage(x, "x")
+        _need(w, "w", x.dtype, (None, None, None), x)
+        groups, c_out, c_in = w.shape
+        _need(x, "x", x.dtype, (None, c_in), x)
+        _need(y, "y", x.dtype, (None, c_out), x)
+        _need(starts, "starts", torch.int32, (groups + 1,), x)
+        if b is not None:
+            _need(b, "b", torch.float32, (groups, c_out), x)
+        rows = min(x.shape[0], y.shape[0])
+        for name, t in (("src", src), ("dst", dst)):
+            if t is not None:
+                _need(t, name, torch.int32, (None,), x)
+                rows = t.numel()
+        if src is not None and dst is not None and src.numel() != dst.numel():
+            raise DynconvError("src and dst: %d and %d positions" % (src.numel(), dst.numel()))
+        self.y = y
+        self.keep = (x, y, w, b, starts, src, dst)
+        self.linear = LinearStruct(c_in, c_out, _raw(w), _raw(b), int(act))
+        self._prepare(x.device, lib.dynconv_grouped_linear, "dynconv_grouped_linear",
+                      (_raw(x), x.shape[0], _raw(y), y.shape[0], dtype_code(x.dtype), ctypes.byref(self.linear), groups,
+                       _raw(starts), rows, _raw(src), int(src_div), _raw(dst)))
+
+    def _result(self):
+        return self.y
+
+
+def grouped_linear(x, y, w, b, starts, src=None, src_div=1, dst=None, act=ACT_NONE, stream=None):
+    return _once(GroupedLinear, stream, x, y, w, b, starts, src, src_div, dst, act)
+
+
+@dataclass
+class ExpertWeights:
+    """An expert layer's weights (dynconv_experts): w_expand, w_gate
+    [experts, hidden, c_in], w_project [experts, c_out, hidden] in the storage
+    dtype; fp32 biases or None."""
+
+    w_expand: torch.Tensor
+    w_project: torch.Tensor
+    w_gate: torch.Tensor = None
+    b_expand: torch.Tensor = None
+    b_gate: torch.Tensor = None
+    b_project: torch.Tensor = None
+    act: int = ACT_SILU
+
+    def check(self, x):
+        _need(self.w_expand, "w_expand", x.dtype, (None, None, None), x)
+        n, h, c = self.w_expand.shape
+        _need(x, "x", x.dtype, (None, c), x)
+        _need(self.w_project, "w_project", x.dtype, (n, None, h), x)
+        if self.w_gate is not None:
+            _need(self.w_gate, "w_gate", x.dtype, (n, h, c), x)
+        elif self.b_gate is not None:
+            raise DynconvError("b_gate without w_gate")
+        for name, width in (("b_expand", h), ("b_gate", h), ("b_project", self.w_project.shape[1])):
+            t = getattr(self, name)
+            if t is not None:
+                _need(t, name, torch.float32, (n, width), x)
+
+    def struct(self) -> ExpertsStruct:
+        n, h, c = self.w_expand.shape
+        return ExpertsStruct(c, h, self.w_project.shape[1], n, _raw(self.w_expand), _raw(self.b_expand),
+                             _raw(self.w_gate), _raw(self.b_gate), _raw(self.w_project), _raw(self.b_project),
+                             int(self.act))
+
+
+class Experts(_Prepared):
+    """A prepared dynconv_experts_forward call; y may be x (in place)."""
+
+    def __init__(self, x, y, weights: ExpertWeights, routes: Routes, flags=0, ws=None):
+        lib = load()
+        _storage(x, "x")
+        weights.check(x)
+        tokens, experts = x.shape[0], weights.w_expand.shape[0]
+        _need(y, "y", x.dtype, (tokens, weights.w_project.shape[1]), x)
+        top_k = routes.expert.shape[-1]
+        routes.check(tokens, experts, top_k, x)
+        self.struct, self.rstruct = weights.struct(), routes.struct()
+        code = dtype_code(x.dtype)
+        nbytes = lib.dynconv_experts_workspace_bytes(tokens, ctypes.byref(self.struct), code, top_k)
+        self.ws = _scratch(nbytes, ws, x.device, "dynconv_experts_workspace_bytes")
+        self.y = y
+        self.keep = (x, y, weights, routes)
+        self._prepare(x.device, lib.dynconv_experts_forward, "dynconv_experts_forward",
+                      (_raw(x), _raw(y), tokens, code, ctypes.byref(self.struct), top_k, ctypes.byref(self.rstruct),
+                       int(flags), self.ws.data_ptr(), self.ws.numel() * self.ws.element_size()))
+
+    def _result(self):
+        return self.y
+
+
+def experts_forward(x, y, weights: ExpertWeights, routes: Routes, flags=0, stream=None):
+    return _once(Experts, stream, x, y, weights, routes, flags)
+
+
+@dataclass
+class Adapters:
+    """Low-rank adapters (dynconv_adapters): down [n, max_rank, c_in], up
+    [n, c_out, max_rank] in the storage dtype, scales fp32 [n] or None, ranks
+    int32 [n] or None."""
+
+    down: torch.Tensor
+    up: torch.Tensor
+    scales: torch.Tensor = None
+    ranks: torch.Tensor = None
+
+    def check(self, x, c_out):
+        _need(self.down, "down", x.dtype, (None, None, x.shape[1]), x)
+        n, rank, _ = self.down.shape
+        _need(self.up, "up", x.dtype, (n, c_out, rank), x)
+        if self.scales is not None:
+            _need(self.scales, "scales", torch.float32, (n,), x)
+        if self.ranks is not None:
+            _need(self.ranks, "ranks", torch.int32, (n,), x)
+
+    def struct(self) -> AdaptersStruct:
+        return AdaptersStruct(self.down.shape[0], self.down.shape[1], _raw(self.down), _raw(self.up), _raw(self.ranks),
+                              _raw(self.scales))
+
+
+class AdapterLinear(_Prepared):
+    """A prepared dynconv_adapter_linear call:
+    y[r] = act(w x[r] + b + scales[i] * up[i] (down[i] x[r])), i = ids[r]."""
+
+    def __init__(self, x, y, w, b, adapters: Adapters, ids, act=ACT_NONE, ws=None):
+        lib = load()
+        _storage(x, "x")
+        _need(w, "w", x.dtype, (None, None), x)
+        c_out, c_in = w.shape
+        _need(x, "x", x.dtype, (None, c_in), x)
+        rows = x.shape[0]
+        _need(y, "y", x.dtype, (rows, c_out), x)
+        _need(ids, "ids", torch.int32, (rows,), x)
+        if b is not None:
+            _need(b, "b", torch.float32, (c_out,), x)
+        adapters.check(x, c_out)
+        self.linear, self.struct = LinearStruct(c_in, c_out, _raw(w), _raw(b), int(act)), adapters.struct()
+        code = dtype_code(x.dtype)
+        nbytes = lib.dynconv_adapter_workspace_bytes(rows, ctypes.byref(self.linear), ctypes.byref(self.struct), code)
+        self.ws = _scratch(nbytes, ws, x.device, "dynconv_adapter_workspace_bytes")
+        self.y = y
+        self.keep = (x, y, w, b, adapters, ids)
+        self._prepare(x.device, lib.dynconv_adapter_linear, "dynconv_adapter_linear",
+                      (_raw(x), _raw(y), rows, code, ctypes.byref(self.linear), ctypes.byref(self.struct), _raw(ids),
+                       self.ws.data_ptr(), self.ws.numel() * self.ws.element_size()))
+
+    def _result(self):
+        return self.y
+
+
+def adapter_linear(x, y, w, b, adapters: Adapters, ids, act=ACT_NONE, stream=None):
+    return _once(AdapterLinear, stream, x, y, w, b, adapters, ids, act)
