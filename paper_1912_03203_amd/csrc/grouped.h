@@ -13,7 +13,10 @@
 // rows the B operand, so a lane ends with 4 consecutive outputs of one row.
 #pragma once
 
+#include <type_traits>
+
 #include "kernels.h"
+#include "wide.h"
 
 namespace dynconv {
 
@@ -73,49 +76,86 @@ struct RowsArgs {
 };
 
 // ---------------------------------------------------------------- tiles
-// Tile `tile` of the groups' rows in tiles of BM: its group and rows, false
-// past the last tile.  Every wave works it out by itself, 64 groups a step.
+// Work item `id` of the launch: a tile of BM rows of one group (group, row0,
+// end) and a slice of the outputs; false past the last one.  Every wave works
+// it out by itself, 64 groups a step: the tiles that the groups really have,
+// then the item's place among them.  Workgroups go to the 8 XCDs in turn, so
+// an XCD gets one run of the items: its L2 then holds the rows and weights of
+// neighbouring tiles.  Within a run 8 slices of a row tile come side by side.
 struct RowTile {
-    int group;
+    int group, slice;
     int64_t row0, end;
 };
 
 __device__ __forceinline__ int64_t clamp_row(int64_t v, int64_t rows) { return v < 0 ? 0 : v > rows ? rows : v; }
 
+constexpr int kBand = 8;
+
 template <int BM>
-__device__ __forceinline__ bool find_tile(const int32_t *__restrict__ starts, int groups, int64_t rows, int tile,
-                                          RowTile &t) {
+__device__ __forceinline__ int group_tiles(const int32_t *__restrict__ starts, int groups, int64_t rows, int g, int &lo,
+                                           int &hi) {
+    lo = hi = 0;
+    if (g < groups) {
+        lo = static_cast<int>(clamp_row(starts[g], rows));
+        hi = static_cast<int>(clamp_row(starts[g + 1], rows));
+    }
+    return hi > lo ? static_cast<int>((static_cast<int64_t>(hi) - lo + BM - 1) / BM) : 0;
+}
+
+__device__ __forceinline__ int wave_incl(int v, int lane) {
+#pragma unroll
+    for (int d = 1; d < kWave; d <<= 1) {
+        const int o = __shfl_up(v, d);
+        if (lane >= d) v += o;
+    }
+    return v;
+}
+
+template <int BM>
+__device__ __forceinline__ bool find_tile(const int32_t *__restrict__ starts, int groups, int64_t rows, int id,
+                                          int slices, RowTile &t) {
+    const int lane = threadIdx.x % kWave;
+    int lo = 0, hi = 0, incl = 0, n = 0;
+    int64_t total;
+    if (!starts) {
+        total = (rows + BM - 1) / BM;
+    } else {
+        int sum = 0;
+        for (int g0 = 0; g0 < groups; g0 += kWave) {
+            n = group_tiles<BM>(starts, groups, rows, g0 + lane, lo, hi);
+            incl = wave_incl(n, lane);
+            sum += __builtin_amdgcn_readlane(incl, kWave - 1);
+        }
+        total = sum;
+    }
+    // fewer than 2^31 items: the host refuses more
+    const uint32_t tiles = static_cast<uint32_t>(total), items = tiles * slices, per = (items + 7) / 8;
+    const uint32_t place = static_cast<uint32_t>(id) / 8, item = static_cast<uint32_t>(id) % 8 * per + place;
+    if (place >= per || item >= items) return false;
+    const int band = slices > kBand ? static_cast<int>(item / (tiles * kBand)) : 0;
+    const int width = slices - band * kBand < kBand ? slices - band * kBand : kBand;
+    const uint32_t in_band = item - tiles * kBand * band;
+    const int tile = static_cast<int>(in_band / static_cast<uint32_t>(width));
+    t.slice = band * kBand + static_cast<int>(in_band % static_cast<uint32_t>(width));
     if (!starts) {
         t.group = 0;
         t.row0 = static_cast<int64_t>(tile) * BM;
         t.end = rows;
-        return t.row0 < rows;
+        return true;
     }
-    const int lane = threadIdx.x % kWave;
     int before = 0;
     for (int g0 = 0; g0 < groups; g0 += kWave) {
-        const int g = g0 + lane;
-        int64_t lo = 0, hi = 0;
-        if (g < groups) {
-            lo = clamp_row(starts[g], rows);
-            hi = clamp_row(starts[g + 1], rows);
-        }
-        const int n = hi > lo ? static_cast<int>((hi - lo + BM - 1) / BM) : 0;
-        int incl = n;
-#pragma unroll
-        for (int d = 1; d < kWave; d <<= 1) {
-            const int o = __shfl_up(incl, d);
-            if (lane >= d) incl += o;
+        if (groups > kWave) {
+            n = group_tiles<BM>(starts, groups, rows, g0 + lane, lo, hi);
+            incl = wave_incl(n, lane);
         }
         const uint64_t past = __ballot(before + incl > tile);
         if (past) {
             const int l = __ffsll(static_cast<unsigned long long>(past)) - 1;
             t.group = g0 + l;
-            const int lo32 = __builtin_amdgcn_readlane(static_cast<int>(lo), l);
-            const int hi32 = __builtin_amdgcn_readlane(static_cast<int>(hi), l);
             const int first = before + __builtin_amdgcn_readlane(incl - n, l);
-            t.row0 = static_cast<int64_t>(lo32) + static_cast<int64_t>(tile - first) * BM;
-            t.end = hi32;
+            t.row0 = static_cast<int64_t>(__builtin_amdgcn_readlane(lo, l)) + static_cast<int64_t>(tile - first) * BM;
+            t.end = __builtin_amdgcn_readlane(hi, l);
             return true;
         }
         before += __builtin_amdgcn_readlane(incl, kWave - 1);
@@ -232,8 +272,8 @@ k_rows_few(RowsArgs a, int slices) {
     const int r = lane % 16, g = lane / 16;
     const int id = block_xy();
     RowTile t;
-    if (!find_tile<BM>(a.starts, a.groups, a.rows, id / slices, t)) return;
-    const int n0 = id % slices * 16;
+    if (!find_tile<BM>(a.starts, a.groups, a.rows, id, slices, t)) return;
+    const int n0 = t.slice * 16;
     const int n = n0 + r < a.c_out ? n0 + r : a.c_out - 1;
     const int64_t woff = (static_cast<int64_t>(t.group) * a.c_out + n) * a.pitch;
     const char *wp[NF];
@@ -325,158 +365,176 @@ k_rows_few(RowsArgs a, int slices) {
 }
 
 // ------------------------------------------------------------- many rows
-// Tiles of BM rows x BN outputs through LDS, 128 bytes of the contraction a
-// step.  A row's 8 chunks are stored at chunk ^ (row % 8), so the 16 rows that
-// a wave reads at one chunk spread over all banks; the loads go straight to
+// Tiles of BM rows x BN outputs through LDS, 64 bytes of the contraction a
+// step, four steps of LDS: the loads of three steps are in flight or landed
+// while one is multiplied.  A row's 4 chunks are stored at chunk ^ (row / 2 % 4),
+// so 8 neighbouring rows at one chunk cover all banks; the loads go straight to
 // LDS, which fixes a lane's place there, so the swizzle is applied to the
-// address that each lane loads.  Two buffers: a step's loads are in flight
-// while the step before is multiplied.  Gated: the outputs of a tile are 16 of
-// the value's and 16 of the gate's in turn, so a wave holds both.
+// address that each lane loads.  Gated: the outputs of a tile are 16 of the
+// value's and 16 of the gate's in turn, so a wave holds both.
+//
+// Tiles of 8 waves run as two groups of four (one wave a SIMD each), half a
+// step apart: while one group multiplies, the other reads its operands from
+// LDS.  Smaller tiles leave that to the several workgroups of a CU.
 __device__ const u32x4 kZeroChunk[1] = {u32x4{0, 0, 0, 0}};
 
 template <int BM, int BN>
 struct TileCfg {
-    static constexpr int kWavesM = 2, kWavesN = BN / 64;
+    static constexpr int kWavesM = 2, kWavesN = BN >= 256 ? 4 : 2;
     static constexpr int kWaves = kWavesM * kWavesN;
     static constexpr int kThreads = kWaves * kWave;
+    static constexpr bool kTwo = kWaves == 8;
     static constexpr int kMF = BM / kWavesM / 16, kNF = BN / kWavesN / 16;
-    static constexpr int kLoadsX = BM / 8 / kWaves, kLoadsW = BN / 8 / kWaves;  // of 8 rows, per wave and step
-    static constexpr int kBuffer = (BM + BN) * 128;
+    static constexpr int kLoadsX = BM / 16 / kWaves, kLoadsW = BN / 16 / kWaves;  // of 16 rows, per wave and step
+    static constexpr int kLoads = kLoadsX + kLoadsW;
+    static constexpr int kSlots = 4;
+    static constexpr int kSlot = (BM + BN) * 64;
+    static constexpr int kWpe = kTwo ? 2 : BM >= 128 ? 2 : 4;  // waves a SIMD that the registers must allow
 };
 
-// 16 bytes a lane from global memory straight to LDS at `to` + 16 * lane.  As
+// 16 bytes a lane from global memory straight to LDS at `to` + OFF + 16 * lane.  As
 // assembly, because the compiler otherwise waits for the loads in flight to
 // the other buffer before each read of LDS; loads_barrier does all the waiting.
+// The readfirstlanes sit in the operands: without optimisation, variables would
+// come back from the stack as vector registers.
+#define DC_UNIFORM(v) __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(v))
+template <int OFF>
 __device__ __forceinline__ void load_to_lds(const char *from, uint32_t to) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to), "v"(from));
+    asm volatile("s_add_u32 m0, %0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(DC_UNIFORM(to)), "v"(from),
+                 "n"(OFF)
+                 : "scc");
 }
-__device__ __forceinline__ void load_to_lds(const char *base, uint32_t off, uint32_t to) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(off), "s"(base));
+#undef DC_UNIFORM
+
+// f(0), f(1), .. f(N - 1) with compile-time numbers
+template <int N, typename F>
+__device__ __forceinline__ void unrolled(F f) {
+    if constexpr (N > 0) {
+        unrolled<N - 1>(f);
+        f(std::integral_constant<int, N - 1>{});
+    }
 }
 
-// Every wave's loads to LDS have landed (they count as vector memory) and its
-// reads of LDS are done.
+// All but the newest N of this wave's loads have landed, and its reads of LDS
+// are done; then the barrier.
+template <int N>
 __device__ __forceinline__ void loads_barrier() {
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    static_assert(N < 64, "the counter has 6 bits");
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
 }
-
-// No load to LDS may be under way when a workgroup ends and gives its LDS back.
-__device__ __forceinline__ void loads_landed() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
-
-template <typename P>
-__device__ __forceinline__ P uniform_ptr(P p) {
-    const uint64_t u = reinterpret_cast<uint64_t>(p);
-    const uint32_t lo = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(u));
-    const uint32_t hi = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(u >> 32));
-    return reinterpret_cast<P>((static_cast<uint64_t>(hi) << 32) | lo);
-}
-
 template <typename T, typename OT, int BM, int BN, bool GATED, bool ADAPT>
-__global__ void __launch_bounds__((TileCfg<BM, BN>::kThreads)) __attribute__((amdgpu_waves_per_eu(2, 2)))
+__global__ void __launch_bounds__((TileCfg<BM, BN>::kThreads))
+__attribute__((amdgpu_waves_per_eu(TileCfg<BM, BN>::kWpe, TileCfg<BM, BN>::kWpe)))
 k_rows_tile(RowsArgs a, int slices) {
     typedef TileCfg<BM, BN> C;
     constexpr int MF = C::kMF, NF = C::kNF;
-    __shared__ __attribute__((aligned(1024))) char lds[2 * C::kBuffer];
+    __shared__ __attribute__((aligned(1024))) char lds[C::kSlots * C::kSlot];
     const uint32_t lds0 = static_cast<uint32_t>(
         reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) char *)(lds)));
     const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const int r = lane % 16, g = lane / 16;
-    const int id = block_xy();
     RowTile t;
-    if (!find_tile<BM>(a.starts, a.groups, a.rows, id / slices, t)) return;
+    if (!find_tile<BM>(a.starts, a.groups, a.rows, block_xy(), slices, t)) return;
     constexpr int kOuts = GATED ? BN / 2 : BN;  // outputs of a tile
-    const int n0 = id % slices * kOuts;
+    const int n0 = t.slice * kOuts;
 
-    // this lane's chunks: row 8 i + lane / 8 of the tile, place lane % 8
-    const int lrow = lane / 8, lchunk = (lane % 8) ^ lrow;
-    const char *xp[C::kLoadsX];
-    uint32_t wo[C::kLoadsW];
+    // this lane's next chunks: row 16 i + lane / 4 of the tile, place lane % 4;
+    // the rows that go in first, then the weights
+    const int lrow = lane / 4, lchunk = (lane % 4) ^ (lrow / 2 % 4);
+    const char *next[C::kLoads];
 #pragma unroll
     for (int i = 0; i < C::kLoadsX; ++i) {
-        const int64_t p = t.row0 + (wave * C::kLoadsX + i) * 8 + lrow;
+        const int64_t p = t.row0 + (wave * C::kLoadsX + i) * 16 + lrow;
         const int64_t s = p < t.end ? source_row(a, p) : -1;
-        xp[i] = a.x + (s < 0 ? 0 : s) * a.pitch + lchunk * 16;
+        next[i] = a.x + (s < 0 ? 0 : s) * a.pitch + lchunk * 16;
     }
 #pragma unroll
     for (int i = 0; i < C::kLoadsW; ++i) {
-        const int j = (wave * C::kLoadsW + i) * 8 + lrow;
-        int n = GATED ? j / 32 * 16 + j % 16 : j;
-        n = n0 + n < a.c_out ? n : a.c_out - 1 - n0;
-        wo[i] = static_cast<uint32_t>(n) * static_cast<uint32_t>(a.pitch) + lchunk * 16;
+        const int j = wave * C::kLoadsW + i;  // 16 rows of the weights' tile
+        const int n = n0 + (GATED ? j / 2 : j) * 16 + lrow;
+        next[C::kLoadsX + i] = (GATED && j % 2 ? a.w2 : a.w) +
+                               (static_cast<int64_t>(t.group) * a.c_out + (n < a.c_out ? n : a.c_out - 1)) * a.pitch +
+                               lchunk * 16;
     }
-    const int64_t woff = (static_cast<int64_t>(t.group) * a.c_out + n0) * a.pitch;
-    const char *wb = uniform_ptr(a.w + woff), *wb2 = GATED ? uniform_ptr(a.w2 + woff) : wb;
-    const int steps = static_cast<int>((a.pitch + 127) / 128), whole = static_cast<int>(a.pitch / 128);
-    const uint32_t xl = lds0 + wave * C::kLoadsX * 1024, wl = lds0 + BM * 128 + wave * C::kLoadsW * 1024;
+    const int own_steps = static_cast<int>((a.pitch + 63) / 64);
+    int steps = own_steps, left = static_cast<int>(a.pitch) - lchunk * 16;  // bytes of the row from this lane's chunk on
+    const uint32_t xl = lds0 + wave * C::kLoadsX * 1024, wl = lds0 + BM * 64 + wave * C::kLoadsW * 1024;
     const char *zero = reinterpret_cast<const char *>(kZeroChunk);
     // The adapters: each distinct one of the tile's rows is more steps of the
     // contraction, v against up, with the other adapters' rows at zero.
     constexpr int kPer = 16 / static_cast<int>(sizeof(T));
     int open[BM / kWave], ad = -1, rank = 0, k0 = 0;
-    if constexpr (ADAPT) {
+    auto next_adapter = [&]() {
+        ad = -1;
+#pragma unroll
+        for (int i = 0; i < BM / kWave; ++i) {
+            const uint64_t left = __ballot(open[i] >= 0);
+            if (left && ad < 0)
+                ad = __builtin_amdgcn_readlane(open[i], __ffsll(static_cast<unsigned long long>(left)) - 1);
+        }
+        if (ad < 0) return false;
+#pragma unroll
+        for (int i = 0; i < BM / kWave; ++i) open[i] = open[i] == ad ? -1 : open[i];
+        rank = adapter_rank(a, ad);
+        k0 = 0;
+        return true;
+    };
+    auto open_adapters = [&]() {
 #pragma unroll
         for (int i = 0; i < BM / kWave; ++i) {
             const int64_t p = t.row0 + i * kWave + lane;
             open[i] = adapter_of(a, p, p < t.end);
         }
-    }
-    auto next_adapter = [&]() {
-        k0 += 8 * kPer;
-        while (k0 >= rank) {
-            ad = -1;
-#pragma unroll
-            for (int i = 0; i < BM / kWave; ++i) {
-                const uint64_t left = __ballot(open[i] >= 0);
-                if (left && ad < 0)
-                    ad = __builtin_amdgcn_readlane(open[i], __ffsll(static_cast<unsigned long long>(left)) - 1);
-            }
-            if (ad < 0) return false;
-#pragma unroll
-            for (int i = 0; i < BM / kWave; ++i) open[i] = open[i] == ad ? -1 : open[i];
-            rank = adapter_rank(a, ad);
-            k0 = 0;
-        }
-        return true;
     };
-    // the loads of step `step`; past the last step zeros, and false
-    auto load = [&](int step, uint32_t buf) {
-        const int64_t off = static_cast<int64_t>(step) * 128;
-        if (step < whole) {
+    if constexpr (ADAPT) {
+        open_adapters();
+        while (next_adapter())
+            if (rank > 0) steps += (rank + 4 * kPer - 1) / (4 * kPer);
+        open_adapters();
+        rank = 0;
+    }
+    // Where the loads of step `step` come from; past the last step zeros.  The
+    // steps are taken in order.
+    const char *from[C::kLoads];
+    auto sources = [&](int step) {
 #pragma unroll
-            for (int i = 0; i < C::kLoadsX; ++i) load_to_lds(xp[i] + off, xl + buf + i * 1024);
-#pragma unroll
-            for (int i = 0; i < C::kLoadsW; ++i)
-                load_to_lds((GATED && ((wave * C::kLoadsW + i) & 2) ? wb2 : wb) + off, wo[i], wl + buf + i * 1024);
-            return true;
+        for (int i = 0; i < C::kLoads; ++i) {
+            from[i] = left > 0 ? next[i] : zero;
+            next[i] += 64;
         }
+        left -= 64;
         if constexpr (ADAPT) {
-            if (step >= steps && next_adapter()) {
+            if (step >= own_steps && step < steps) {
+                while (k0 >= rank)
+                    if (!next_adapter()) break;
                 const int k = k0 + lchunk * kPer;
                 const T *up = reinterpret_cast<const T *>(a.up) + static_cast<int64_t>(ad) * a.c_out * a.max_rank + k;
 #pragma unroll
                 for (int i = 0; i < C::kLoadsX; ++i) {
-                    const int64_t p = t.row0 + (wave * C::kLoadsX + i) * 8 + lrow;
+                    const int64_t p = t.row0 + (wave * C::kLoadsX + i) * 16 + lrow;
                     const bool in = k < rank && adapter_of(a, p, p < t.end) == ad;
-                    load_to_lds(in ? a.v + p * a.v_pitch + k * static_cast<int>(sizeof(T)) : zero, xl + buf + i * 1024);
+                    from[i] = in ? a.v + p * a.v_pitch + k * static_cast<int>(sizeof(T)) : zero;
                 }
 #pragma unroll
                 for (int i = 0; i < C::kLoadsW; ++i) {
-                    int n = n0 + (wave * C::kLoadsW + i) * 8 + lrow;
+                    int n = n0 + (wave * C::kLoadsW + i) * 16 + lrow;
                     n = n < a.c_out ? n : a.c_out - 1;
-                    load_to_lds(k < rank ? reinterpret_cast<const char *>(up + static_cast<int64_t>(n) * a.max_rank) : zero,
-                                wl + buf + i * 1024);
+                    from[C::kLoadsX + i] =
+                        k < rank ? reinterpret_cast<const char *>(up + static_cast<int64_t>(n) * a.max_rank) : zero;
                 }
-                return true;
+                k0 += 4 * kPer;
             }
         }
-        const bool in = off + lchunk * 16 < a.pitch;
-#pragma unroll
-        for (int i = 0; i < C::kLoadsX; ++i) load_to_lds(in ? xp[i] + off : zero, xl + buf + i * 1024);
-#pragma unroll
-        for (int i = 0; i < C::kLoadsW; ++i)
-            load_to_lds(in ? (GATED && ((wave * C::kLoadsW + i) & 2) ? wb2 : wb) + off + wo[i] : zero,
-                        wl + buf + i * 1024);
-        return step < steps;
+    };
+    auto load = [&](int step, auto at) {  // one of the step's loads
+        constexpr int i = decltype(at)::value;
+        const uint32_t slot = static_cast<uint32_t>(step % C::kSlots) * C::kSlot;
+        if constexpr (i < C::kLoadsX) load_to_lds<i * 1024>(from[i], xl + slot);
+        else load_to_lds<(i - C::kLoadsX) * 1024>(from[i], wl + slot);
+    };
+    auto load_all = [&](int step) {
+        sources(step);
+        unrolled<C::kLoads>([&](auto i) { load(step, i); });
     };
 
     const int wm = wave % C::kWavesM * (BM / C::kWavesM), wn = wave / C::kWavesM * (BN / C::kWavesN);
@@ -485,51 +543,126 @@ k_rows_tile(RowsArgs a, int slices) {
     for (int i = 0; i < NF; ++i)
 #pragma unroll
         for (int f = 0; f < MF; ++f) acc[i][f] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
-    const char *xr = lds + (wm + r) * 128, *wr = lds + (BM + wn + r) * 128;
-    auto multiply = [&](int buf) {
+    const int chunk = (g ^ (r / 2 % 4)) * 16;
+    const char *xr = lds + (wm + r) * 64 + chunk, *wr = lds + (BM + wn + r) * 64 + chunk;
+    u32x4 xv[MF], wv[NF];
+    auto read = [&](int step) {
+        const int slot = step % C::kSlots * C::kSlot;
 #pragma unroll
-        for (int kk = 0; kk < 2; ++kk) {
-            u32x4 xv[MF], wv[NF];
-            const int chunk = ((kk * 4 + g) ^ (r & 7)) * 16 + buf;
+        for (int i = 0; i < NF; ++i) wv[i] = *reinterpret_cast<const u32x4 *>(wr + slot + i * 1024);
 #pragma unroll
-            for (int i = 0; i < NF; ++i) wv[i] = *reinterpret_cast<const u32x4 *>(wr + i * 2048 + chunk);
+        for (int f = 0; f < MF; ++f) xv[f] = *reinterpret_cast<const u32x4 *>(xr + slot + f * 1024);
+    };
+    auto multiply = [&](auto at) {  // one tile of 16 outputs
+        constexpr int i = decltype(at)::value;
 #pragma unroll
-            for (int f = 0; f < MF; ++f) xv[f] = *reinterpret_cast<const u32x4 *>(xr + f * 2048 + chunk);
+        for (int f = 0; f < MF; ++f) acc[i][f] = chunk_mma<T>(wv[i], xv[f], acc[i][f]);
+    };
+    load_all(0);
+    load_all(1);
+    load_all(2);
+    // where the wave's rows go: lane l has rows l, l + 64, .. of them
+    constexpr int kTargets = (MF * 16 + kWave - 1) / kWave;
+    int target[kTargets];
+#pragma unroll
+    for (int i = 0; i < kTargets; ++i) {
+        const int64_t p = t.row0 + wm + i * kWave + lane;
+        const bool have = i * kWave + lane < MF * 16 && p < t.end;
+        target[i] = have && source_row(a, p) >= 0 ? static_cast<int>(target_row(a, p)) : -1;
+    }
+    if constexpr (C::kTwo) {
+        const bool second = wave >= C::kWaves / 2;
+        loads_barrier<2 * C::kLoads>();
+        if (second) __builtin_amdgcn_s_barrier();
+        for (int s = 0; s < steps; ++s) {
+            read(s);
+            __builtin_amdgcn_sched_barrier(0);
+            loads_barrier<C::kLoads>();  // step s + 1 has landed, step s + 2 may be under way
+            // Multiplying, and between the products the loads of step s + 3, into
+            // the slot of step s - 1, which both groups have read.
+            __builtin_amdgcn_sched_barrier(0);
+            __builtin_amdgcn_s_setprio(1);
+            sources(s + 3);
+            unrolled<NF>([&](auto i) {
+                multiply(i);
+                __builtin_amdgcn_sched_barrier(0);
+                constexpr int per = (C::kLoads + NF - 1) / NF;
+                unrolled<per>([&](auto j) {
+                    constexpr int l = decltype(i)::value * per + decltype(j)::value;
+                    if constexpr (l < C::kLoads) load(s + 3, std::integral_constant<int, l>{});
+                });
+                __builtin_amdgcn_sched_barrier(0);
+            });
+            __builtin_amdgcn_s_setprio(0);
+            __builtin_amdgcn_s_barrier();
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        if (!second) __builtin_amdgcn_s_barrier();
+    } else {
+        for (int s = 0; s < steps; ++s) {
+            loads_barrier<2 * C::kLoads>();  // step s has landed, step s - 1 is read
+            load_all(s + 3);
+            read(s);
+            unrolled<NF>(multiply);
+        }
+    }
+    loads_barrier<0>();  // LDS is free: each wave takes its share for its sums
+
+    // The sums go through LDS in fp32 (16-byte chunk c of a row at c ^ row % 16),
+    // so that a lane finishes 16 bytes of one row and a store covers whole lines,
+    // in a loop that is short code: every workgroup runs it once.
+    constexpr int kCols = NF * 16, kRowBytes = kCols * 4, kChunks = kCols / 4;
+    constexpr int kShare = C::kSlots * C::kSlot / C::kWaves;
+    constexpr int kRows = kShare / kRowBytes < MF * 16 ? kShare / kRowBytes : MF * 16;  // of a pass
+    constexpr int kPerLane = 16 / static_cast<int>(sizeof(OT)), kOut = GATED ? kCols / 2 : kCols;
+    constexpr int kLanes = kOut / kPerLane, kAtOnce = kWave / kLanes;  // lanes of a row, rows of a store
+    char *mine = lds + wave * kShare;
+    const int col = lane % kLanes * kPerLane, n = n0 + (GATED ? wn / 2 : wn) + col;
+    const int c0 = ((GATED ? col / 16 * 32 + col % 16 : col)) / 4;
+    const bool in = n < a.c_out;
+    float bias[kPerLane], bias2[kPerLane];
+#pragma unroll
+    for (int u = 0; u < kPerLane; u += 4) {
+#pragma unroll
+        for (int v = 0; v < 4; ++v) bias[u + v] = bias2[u + v] = 0.0f;
+        const int64_t at = static_cast<int64_t>(t.group) * a.c_out + n + u;
+        if (in && a.b) io<float>::load4(a.b + at, bias + u);
+        if (GATED && in && a.b2) io<float>::load4(a.b2 + at, bias2 + u);
+    }
+    unrolled<MF * 16 / kRows>([&](auto pass) {
+        constexpr int f0 = decltype(pass)::value * (kRows / 16);
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int f = 0; f < kRows / 16; ++f)
 #pragma unroll
             for (int i = 0; i < NF; ++i)
+                *reinterpret_cast<floatx4 *>(mine + (f * 16 + r) * kRowBytes +
+                                             ((i * 4 + g) ^ (r & (kChunks - 1))) * 16) = acc[i][f0 + f];
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll 1
+        for (int row = lane / kLanes; row < kRows; row += kAtOnce) {
+            const int to = __shfl(target[f0 * 16 / kWave], (f0 * 16 + row) % kWave);
+            const char *from_row = mine + row * kRowBytes;
+            float out[kPerLane];
 #pragma unroll
-                for (int f = 0; f < MF; ++f) acc[i][f] = chunk_mma<T>(wv[i], xv[f], acc[i][f]);
+            for (int u = 0; u < kPerLane; u += 4) {
+                const int c = c0 + u / 4;
+                const floatx4 v = *reinterpret_cast<const floatx4 *>(from_row + (c ^ (row & 15 & (kChunks - 1))) * 16);
+                floatx4 w = v;
+                if (GATED)
+                    w = *reinterpret_cast<const floatx4 *>(from_row + ((c + 4) ^ (row & 15 & (kChunks - 1))) * 16);
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    out[u + e] = GATED ? act_any(w[e] + bias2[u + e], a.act) * (v[e] + bias[u + e])
+                                       : act_any(v[e] + bias[u + e], a.act);
+            }
+            if (to >= 0 && in) {
+                OT *y = reinterpret_cast<OT *>(a.y) + static_cast<int64_t>(to) * a.c_out + n;
+                if constexpr (sizeof(OT) == 2) store8<OT>(y, out);
+                else io<OT>::store4(y, out);
+            }
         }
-    };
-    // two steps a turn; past an odd last step comes one of zeros, so that every
-    // product is issued unconditionally
-    bool more = load(0, 0);
-    for (int s = 0; more; s += 2) {
-        loads_barrier();  // this step's loads have landed, the other buffer is read
-        load(s + 1, C::kBuffer);
-        multiply(0);
-        loads_barrier();
-        more = load(s + 2, 0);
-        multiply(C::kBuffer);
-    }
-    loads_landed();
-
-#pragma unroll
-    for (int f = 0; f < MF; ++f) {
-        const int64_t p = t.row0 + wm + f * 16 + r;
-        if (p >= t.end || source_row(a, p) < 0) continue;
-        const int64_t to = target_row(a, p);
-        if (to < 0) continue;
-        OT *y = reinterpret_cast<OT *>(a.y) + to * a.c_out;
-#pragma unroll
-        for (int i = 0; i < NF; i += GATED ? 2 : 1) {
-            const int n = n0 + (GATED ? (wn + i * 16) / 2 : wn + i * 16) + 4 * g;
-            if (n >= a.c_out) continue;
-            float out[4];
-            finish4<GATED>(a, t.group, n, acc[i][f], acc[GATED ? i + 1 : i][f], out);
-            store_out<OT>(y + n, out);
-        }
-    }
+    });
 }
 
 // ------------------------------------------------------- sums of a token

@@ -121,11 +121,13 @@ RowsPlan rows_plan(int64_t rows, int64_t groups, bool split, int c_out, bool gat
         p.bm = mean <= 16 ? 16 : mean <= 32 ? 32 : 64;
         p.slices = (c_out + 15) / 16;
     } else {
-        p.bm = dt != DYNCONV_F32 && mean >= 256 && rows / 256 * c_out / 256 >= 256 ? 256 : 128;
+        const int64_t outs256 = static_cast<int64_t>(c_out) * (gated ? 2 : 1) / 256;
+        p.bm = dt != DYNCONV_F32 && mean >= 256 && rows / 256 * outs256 >= 192 ? 256
+               : rows / 128 * c_out * (gated ? 2 : 1) / 128 >= 256 ? 128 : 64;
         const int outs = gated ? p.bm / 2 : p.bm;
         p.slices = (c_out + outs - 1) / outs;
     }
-    p.blocks = most_tiles(rows, groups, p.bm, split) * p.slices;
+    p.blocks = (most_tiles(rows, groups, p.bm, split) * p.slices + 7) / 8 * 8;  // whole turns of the 8 XCDs
     return p;
 }
 
@@ -146,7 +148,10 @@ void launch_rows(const RowsArgs &a, const RowsPlan &p, hipStream_t st, Marks &mk
             return;
         }
     }
-    launch(mk, k_rows_tile<T, OT, 128, 128, GATED, ADAPT>, grid, dim3(TileCfg<128, 128>::kThreads), 0, st, a, p.slices);
+    if (p.bm == 128)
+        launch(mk, k_rows_tile<T, OT, 128, 128, GATED, ADAPT>, grid, dim3(TileCfg<128, 128>::kThreads), 0, st, a, p.slices);
+    else
+        launch(mk, k_rows_tile<T, OT, 64, 64, GATED, ADAPT>, grid, dim3(TileCfg<64, 64>::kThreads), 0, st, a, p.slices);
 }
 
 // out32: the outputs are fp32 whatever the storage type
