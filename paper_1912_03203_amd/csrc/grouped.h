@@ -366,8 +366,7 @@ k_rows_few(RowsArgs a, int slices) {
 
 // ------------------------------------------------------------- many rows
 // Tiles of BM rows x BN outputs through LDS, 64 bytes of the contraction a
-// step, four steps of LDS: the loads of three steps are in flight or landed
-// while one is multiplied.  A row's 4 chunks are stored at chunk ^ (row / 2 % 4),
+// step, five steps of LDS: the loads run four steps ahead of the products.  A row's 4 chunks are stored at chunk ^ (row / 2 % 4),
 // so 8 neighbouring rows at one chunk cover all banks; the loads go straight to
 // LDS, which fixes a lane's place there, so the swizzle is applied to the
 // address that each lane loads.  Gated: the outputs of a tile are 16 of the
@@ -387,7 +386,7 @@ struct TileCfg {
     static constexpr int kMF = BM / kWavesM / 16, kNF = BN / kWavesN / 16;
     static constexpr int kLoadsX = BM / 16 / kWaves, kLoadsW = BN / 16 / kWaves;  // of 16 rows, per wave and step
     static constexpr int kLoads = kLoadsX + kLoadsW;
-    static constexpr int kSlots = 4;
+    static constexpr int kSlots = 5, kAhead = kSlots - 1;  // steps in LDS, steps that the loads run ahead
     static constexpr int kSlot = (BM + BN) * 64;
     static constexpr int kWpe = kTwo ? 2 : BM >= 128 ? 2 : 4;  // waves a SIMD that the registers must allow
 };
@@ -526,15 +525,17 @@ k_rows_tile(RowsArgs a, int slices) {
             }
         }
     };
-    auto load = [&](int step, auto at) {  // one of the step's loads
-        constexpr int i = decltype(at)::value;
-        const uint32_t slot = static_cast<uint32_t>(step % C::kSlots) * C::kSlot;
-        if constexpr (i < C::kLoadsX) load_to_lds<i * 1024>(from[i], xl + slot);
-        else load_to_lds<(i - C::kLoadsX) * 1024>(from[i], wl + slot);
+    uint32_t to = 0, at = 0;  // the slots that are loaded and read next
+    auto after = [](uint32_t slot) { return slot == (C::kSlots - 1) * C::kSlot ? 0u : slot + C::kSlot; };
+    auto load = [&](auto which) {  // one of a step's loads
+        constexpr int i = decltype(which)::value;
+        if constexpr (i < C::kLoadsX) load_to_lds<i * 1024>(from[i], xl + to);
+        else load_to_lds<(i - C::kLoadsX) * 1024>(from[i], wl + to);
     };
     auto load_all = [&](int step) {
         sources(step);
-        unrolled<C::kLoads>([&](auto i) { load(step, i); });
+        unrolled<C::kLoads>(load);
+        to = after(to);
     };
 
     const int wm = wave % C::kWavesM * (BM / C::kWavesM), wn = wave / C::kWavesM * (BN / C::kWavesN);
@@ -546,21 +547,19 @@ k_rows_tile(RowsArgs a, int slices) {
     const int chunk = (g ^ (r / 2 % 4)) * 16;
     const char *xr = lds + (wm + r) * 64 + chunk, *wr = lds + (BM + wn + r) * 64 + chunk;
     u32x4 xv[MF], wv[NF];
-    auto read = [&](int step) {
-        const int slot = step % C::kSlots * C::kSlot;
+    auto read = [&]() {
 #pragma unroll
-        for (int i = 0; i < NF; ++i) wv[i] = *reinterpret_cast<const u32x4 *>(wr + slot + i * 1024);
+        for (int i = 0; i < NF; ++i) wv[i] = *reinterpret_cast<const u32x4 *>(wr + at + i * 1024);
 #pragma unroll
-        for (int f = 0; f < MF; ++f) xv[f] = *reinterpret_cast<const u32x4 *>(xr + slot + f * 1024);
+        for (int f = 0; f < MF; ++f) xv[f] = *reinterpret_cast<const u32x4 *>(xr + at + f * 1024);
+        at = after(at);
     };
     auto multiply = [&](auto at) {  // one tile of 16 outputs
         constexpr int i = decltype(at)::value;
 #pragma unroll
         for (int f = 0; f < MF; ++f) acc[i][f] = chunk_mma<T>(wv[i], xv[f], acc[i][f]);
     };
-    load_all(0);
-    load_all(1);
-    load_all(2);
+    unrolled<C::kAhead>([&](auto step) { load_all(decltype(step)::value); });
     // where the wave's rows go: lane l has rows l, l + 64, .. of them
     constexpr int kTargets = (MF * 16 + kWave - 1) / kWave;
     int target[kTargets];
@@ -572,37 +571,33 @@ k_rows_tile(RowsArgs a, int slices) {
     }
     if constexpr (C::kTwo) {
         const bool second = wave >= C::kWaves / 2;
-        loads_barrier<2 * C::kLoads>();
+        loads_barrier<(C::kAhead - 1) * C::kLoads>();
         if (second) __builtin_amdgcn_s_barrier();
+        sources(C::kAhead);
         for (int s = 0; s < steps; ++s) {
-            read(s);
+            // Reading, and the loads of step s + kAhead, into the slot of step
+            // s - 1, which both groups have read.  (Among the products the loads
+            // hold up: a wave that waits for its turn to load cannot multiply.)
+            read();
+            unrolled<C::kLoads>(load);
+            to = after(to);
             __builtin_amdgcn_sched_barrier(0);
-            loads_barrier<C::kLoads>();  // step s + 1 has landed, step s + 2 may be under way
-            // Multiplying, and between the products the loads of step s + 3, into
-            // the slot of step s - 1, which both groups have read.
+            loads_barrier<(C::kAhead - 1) * C::kLoads>();  // step s + 1 has landed
             __builtin_amdgcn_sched_barrier(0);
             __builtin_amdgcn_s_setprio(1);
-            sources(s + 3);
-            unrolled<NF>([&](auto i) {
-                multiply(i);
-                __builtin_amdgcn_sched_barrier(0);
-                constexpr int per = (C::kLoads + NF - 1) / NF;
-                unrolled<per>([&](auto j) {
-                    constexpr int l = decltype(i)::value * per + decltype(j)::value;
-                    if constexpr (l < C::kLoads) load(s + 3, std::integral_constant<int, l>{});
-                });
-                __builtin_amdgcn_sched_barrier(0);
-            });
+            sources(s + 1 + C::kAhead);
+            unrolled<NF>(multiply);
             __builtin_amdgcn_s_setprio(0);
+            __builtin_amdgcn_sched_barrier(0);
             __builtin_amdgcn_s_barrier();
             __builtin_amdgcn_sched_barrier(0);
         }
         if (!second) __builtin_amdgcn_s_barrier();
     } else {
         for (int s = 0; s < steps; ++s) {
-            loads_barrier<2 * C::kLoads>();  // step s has landed, step s - 1 is read
-            load_all(s + 3);
-            read(s);
+            loads_barrier<(C::kAhead - 1) * C::kLoads>();  // step s has landed, step s - 1 is read
+            load_all(s + C::kAhead);
+            read();
             unrolled<NF>(multiply);
         }
     }
@@ -613,7 +608,8 @@ k_rows_tile(RowsArgs a, int slices) {
     // in a loop that is short code: every workgroup runs it once.
     constexpr int kCols = NF * 16, kRowBytes = kCols * 4, kChunks = kCols / 4;
     constexpr int kShare = C::kSlots * C::kSlot / C::kWaves;
-    constexpr int kRows = kShare / kRowBytes < MF * 16 ? kShare / kRowBytes : MF * 16;  // of a pass
+    constexpr int kRows = MF * 16 < 64 ? MF * 16 : 64;  // of a pass
+    static_assert(kRows * kRowBytes <= kShare && MF * 16 % kRows == 0, "a pass fits the wave's share");
     constexpr int kPerLane = 16 / static_cast<int>(sizeof(OT)), kOut = GATED ? kCols / 2 : kCols;
     constexpr int kLanes = kOut / kPerLane, kAtOnce = kWave / kLanes;  // lanes of a row, rows of a store
     char *mine = lds + wave * kShare;
