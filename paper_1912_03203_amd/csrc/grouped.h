@@ -16,6 +16,7 @@
 #include <type_traits>
 
 #include "kernels.h"
+#include "route.h"
 #include "wide.h"
 
 namespace dynconv {
@@ -72,7 +73,7 @@ struct RowsArgs {
     int v_pitch;
     const char *up;        // [adapters][c_out][max_rank]
     const int32_t *ids, *ranks;
-    int adapters, max_rank;
+    int adapters, max_rank, id_bits;  // id_bits: of the numbers below adapters
 };
 
 // ---------------------------------------------------------------- tiles
@@ -207,189 +208,69 @@ __device__ __forceinline__ int adapter_of(const RowsArgs &a, int64_t row, bool i
     return id >= 0 && id < a.adapters ? id : -1;
 }
 
-// acc += up[id] * v over the distinct adapters of the wave's rows (MF tiles of
-// 16 from row0; id[f]: the adapter of row f * 16 + lane % 16, or -1) and NF
-// tiles of 16 outputs from n0.  Each adapter is one more run of the
-// contraction, with the rows of the others at zero.  Only every `of`-th
-// adapter from `first` is taken (waves that split the work).
-template <typename T, int NF, int MF>
-__device__ __forceinline__ void add_adapters(const RowsArgs &a, const int (&id)[MF], int64_t row0, int n0, int first,
-                                             int of, floatx4 (&acc)[NF][MF]) {
+// The distinct adapters of up to 64 rows, row l's (or -1) in lane l: the lanes
+// that hold the first row of each.
+__device__ __forceinline__ uint64_t distinct_lanes(int id, int bits) {
+    const int lane = threadIdx.x % kWave;
+    const uint64_t same = equal_lanes(static_cast<uint32_t>(id), bits, __ballot(id >= 0));
+    return __ballot(id >= 0 && (same & lanemask_lt(lane)) == 0);
+}
+__device__ __forceinline__ uint64_t drop_lanes(uint64_t set, int n) {
+    for (int i = 0; i < n && set; ++i) set &= set - 1;
+    return set;
+}
+
+// acc += up[id] * v over the distinct adapters of MF * 16 rows from row0 (row
+// l's adapter, or -1, in lane l) and the 16 outputs from n0.  Each adapter is one
+// more run of the contraction, with the rows of the others at zero; of the
+// adapters, every `of`-th from `first` is taken (waves share the work), four at a
+// time, so that the loads of four are in flight.
+template <typename T, int MF>
+__device__ __forceinline__ void add_adapters(const RowsArgs &a, int row_id, int64_t row0, int n0, int first, int of,
+                                             floatx4 (&acc)[1][MF]) {
+    constexpr int kPer = 16 / static_cast<int>(sizeof(T)), kOnce = 4;
     const int lane = threadIdx.x % kWave, g = lane / 16, r = lane % 16;
-    constexpr int kPer = 16 / static_cast<int>(sizeof(T));
-    const char *v = a.v + row0 * a.v_pitch;
-    bool open[MF];
+    uint64_t left = drop_lanes(distinct_lanes(row_id, a.id_bits), first);
+    int id[MF];
 #pragma unroll
-    for (int f = 0; f < MF; ++f) open[f] = id[f] >= 0;
-    for (int turn = 0;; ++turn) {
-        int ad = -1;
-#pragma unroll
-        for (int f = MF - 1; f >= 0; --f) {
-            const uint64_t left = __ballot(open[f]);
-            if (left) ad = __builtin_amdgcn_readlane(id[f], __ffsll(static_cast<unsigned long long>(left)) - 1);
-        }
-        if (ad < 0) break;
-#pragma unroll
-        for (int f = 0; f < MF; ++f) open[f] = open[f] && id[f] != ad;
-        if (turn % of != first) continue;
-        const int rank = adapter_rank(a, ad);
-        const T *up = reinterpret_cast<const T *>(a.up) + static_cast<int64_t>(ad) * a.c_out * a.max_rank;
-        for (int k0 = 0; k0 < rank; k0 += 4 * kPer) {
-            const int k = k0 + g * kPer;
-            u32x4 rv[MF], uv[NF];
-#pragma unroll
-            for (int f = 0; f < MF; ++f) {
-                rv[f] = u32x4{0, 0, 0, 0};
-                if (id[f] == ad && k < rank)
-                    rv[f] = *reinterpret_cast<const u32x4 *>(v + (f * 16 + r) * a.v_pitch + k * static_cast<int>(sizeof(T)));
-            }
-#pragma unroll
-            for (int i = 0; i < NF; ++i) {
-                uv[i] = u32x4{0, 0, 0, 0};
-                const int n = n0 + i * 16 + r;
-                if (k < rank && n < a.c_out)
-                    uv[i] = *reinterpret_cast<const u32x4 *>(up + static_cast<int64_t>(n) * a.max_rank + k);
-            }
-#pragma unroll
-            for (int i = 0; i < NF; ++i)
-#pragma unroll
-                for (int f = 0; f < MF; ++f) acc[i][f] = chunk_mma<T>(uv[i], rv[f], acc[i][f]);
-        }
-    }
-}
-
-// ------------------------------------------------------------- few rows
-// Groups of a few rows: the time is that of reading the weights.  A workgroup
-// takes MF * 16 rows of a group and 16 outputs; its NW waves split the
-// contraction, stream the weights straight into the matrix cores' registers,
-// and add up through LDS in wave order.
-template <typename T, typename OT, int NW, int MF, bool GATED, bool ADAPT>
-__global__ void __launch_bounds__(NW * kWave)
-k_rows_few(RowsArgs a, int slices) {
-    constexpr int BM = MF * 16, NF = GATED ? 2 : 1;
-    __shared__ floatx4 part[NW > 1 ? NW - 1 : 1][NF][MF][kWave];
-    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-    const int r = lane % 16, g = lane / 16;
-    const int id = block_xy();
-    RowTile t;
-    if (!find_tile<BM>(a.starts, a.groups, a.rows, id, slices, t)) return;
-    const int n0 = t.slice * 16;
+    for (int f = 0; f < MF; ++f) id[f] = __shfl(row_id, f * 16 + r);
     const int n = n0 + r < a.c_out ? n0 + r : a.c_out - 1;
-    const int64_t woff = (static_cast<int64_t>(t.group) * a.c_out + n) * a.pitch;
-    const char *wp[NF];
-    wp[0] = a.w + woff;
-    if constexpr (GATED) wp[1] = a.w2 + woff;
-    const char *xp[MF];
-    int64_t from[MF];
+    while (left) {
+        int ad[kOnce], rank[kOnce], most = 0;
 #pragma unroll
-    for (int f = 0; f < MF; ++f) {
-        const int64_t p = t.row0 + f * 16 + r;
-        from[f] = p < t.end ? source_row(a, p) : -1;
-        xp[f] = a.x + (from[f] < 0 ? 0 : from[f]) * a.pitch;
-    }
-    floatx4 acc[NF][MF];
-#pragma unroll
-    for (int i = 0; i < NF; ++i)
-#pragma unroll
-        for (int f = 0; f < MF; ++f) acc[i][f] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
-    // the waves' runs of the contraction, in steps of 64 bytes
-    const int64_t steps = (a.pitch + 63) / 64;
-    const int64_t s0 = steps * wave / NW, s1 = steps * (wave + 1) / NW;
-    constexpr int U = MF == 1 ? 8 : 4;  // steps in flight
-    int64_t s = s0;
-    for (; s + U <= s1 && (s + U) * 64 <= a.pitch; s += U) {
-        u32x4 wv[U][NF], xv[U][MF];
-        const int64_t off = s * 64 + g * 16;
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-#pragma unroll
-            for (int i = 0; i < NF; ++i) wv[u][i] = *reinterpret_cast<const u32x4 *>(wp[i] + off + u * 64);
-#pragma unroll
-            for (int f = 0; f < MF; ++f) xv[u][f] = *reinterpret_cast<const u32x4 *>(xp[f] + off + u * 64);
+        for (int b = 0; b < kOnce; ++b) {
+            ad[b] = left ? __builtin_amdgcn_readlane(row_id, __ffsll(static_cast<unsigned long long>(left)) - 1) : -1;
+            rank[b] = ad[b] < 0 ? 0 : adapter_rank(a, ad[b]);
+            most = rank[b] > most ? rank[b] : most;
+            left = drop_lanes(left, of);
         }
+        for (int k0 = 0; k0 < most; k0 += 4 * kPer) {
+            const int k = k0 + g * kPer;
+            const u32x4 none = {0, 0, 0, 0};
+            u32x4 rv[MF], uv[kOnce];
 #pragma unroll
-        for (int u = 0; u < U; ++u)
+            for (int b = 0; b < kOnce; ++b)
+                uv[b] = k < rank[b] ? *reinterpret_cast<const u32x4 *>(
+                                          a.up + ((static_cast<int64_t>(ad[b]) * a.c_out + n) * a.max_rank + k) *
+                                                     static_cast<int>(sizeof(T)))
+                                    : none;
 #pragma unroll
-            for (int i = 0; i < NF; ++i)
+            for (int f = 0; f < MF; ++f)
+                rv[f] = k < most && id[f] >= 0
+                            ? *reinterpret_cast<const u32x4 *>(a.v + (row0 + f * 16 + r) * a.v_pitch +
+                                                               k * static_cast<int>(sizeof(T)))
+                            : none;
 #pragma unroll
-                for (int f = 0; f < MF; ++f) acc[i][f] = chunk_mma<T>(wv[u][i], xv[u][f], acc[i][f]);
-    }
-    for (; s < s1; ++s) {
-        const int64_t off = s * 64 + g * 16;
-        const bool in = off < a.pitch;
-        u32x4 wv[NF], xv[MF];
+            for (int b = 0; b < kOnce; ++b)
 #pragma unroll
-        for (int i = 0; i < NF; ++i)
-            wv[i] = in ? *reinterpret_cast<const u32x4 *>(wp[i] + off) : u32x4{0, 0, 0, 0};
-#pragma unroll
-        for (int f = 0; f < MF; ++f)
-            xv[f] = in ? *reinterpret_cast<const u32x4 *>(xp[f] + off) : u32x4{0, 0, 0, 0};
-#pragma unroll
-        for (int i = 0; i < NF; ++i)
-#pragma unroll
-            for (int f = 0; f < MF; ++f) acc[i][f] = chunk_mma<T>(wv[i], xv[f], acc[i][f]);
-    }
-    if constexpr (ADAPT) {
-        int ids[MF];
-#pragma unroll
-        for (int f = 0; f < MF; ++f) ids[f] = adapter_of(a, t.row0 + f * 16 + r, t.row0 + f * 16 + r < t.end);
-        add_adapters<T, 1, MF>(a, ids, t.row0, n0, wave, NW, acc);
-    }
-    if (NW > 1) {
-        if (wave > 0) {
-#pragma unroll
-            for (int i = 0; i < NF; ++i)
-#pragma unroll
-                for (int f = 0; f < MF; ++f) part[wave - 1][i][f][lane] = acc[i][f];
+                for (int f = 0; f < MF; ++f)
+                    acc[0][f] = chunk_mma<T>(uv[b], id[f] == ad[b] && k < rank[b] ? rv[f] : none, acc[0][f]);
         }
-        __syncthreads();
-        if (wave > 0) return;
-#pragma unroll
-        for (int w = 0; w < NW - 1; ++w)
-#pragma unroll
-            for (int i = 0; i < NF; ++i)
-#pragma unroll
-                for (int f = 0; f < MF; ++f) acc[i][f] += part[w][i][f][lane];
-    }
-    const int nn = n0 + 4 * g;
-    if (nn >= a.c_out) return;
-#pragma unroll
-    for (int f = 0; f < MF; ++f) {
-        if (from[f] < 0) continue;
-        const int64_t to = target_row(a, t.row0 + f * 16 + r);
-        if (to < 0) continue;
-        float out[4];
-        finish4<GATED>(a, t.group, nn, acc[0][f], acc[NF - 1][f], out);
-        store_out<OT>(reinterpret_cast<OT *>(a.y) + to * a.c_out + nn, out);
     }
 }
 
-// ------------------------------------------------------------- many rows
-// Tiles of BM rows x BN outputs through LDS, 64 bytes of the contraction a
-// step, five steps of LDS: the loads run four steps ahead of the products.  A row's 4 chunks are stored at chunk ^ (row / 2 % 4),
-// so 8 neighbouring rows at one chunk cover all banks; the loads go straight to
-// LDS, which fixes a lane's place there, so the swizzle is applied to the
-// address that each lane loads.  Gated: the outputs of a tile are 16 of the
-// value's and 16 of the gate's in turn, so a wave holds both.
-//
-// Tiles of 8 waves run as two groups of four (one wave a SIMD each), half a
-// step apart: while one group multiplies, the other reads its operands from
-// LDS.  Smaller tiles leave that to the several workgroups of a CU.
+// ------------------------------------------------------------ loads to LDS
 __device__ const u32x4 kZeroChunk[1] = {u32x4{0, 0, 0, 0}};
-
-template <int BM, int BN>
-struct TileCfg {
-    static constexpr int kWavesM = 2, kWavesN = BN >= 256 ? 4 : 2;
-    static constexpr int kWaves = kWavesM * kWavesN;
-    static constexpr int kThreads = kWaves * kWave;
-    static constexpr bool kTwo = kWaves == 8;
-    static constexpr int kMF = BM / kWavesM / 16, kNF = BN / kWavesN / 16;
-    static constexpr int kLoadsX = BM / 16 / kWaves, kLoadsW = BN / 16 / kWaves;  // of 16 rows, per wave and step
-    static constexpr int kLoads = kLoadsX + kLoadsW;
-    static constexpr int kSlots = 5, kAhead = kSlots - 1;  // steps in LDS, steps that the loads run ahead
-    static constexpr int kSlot = (BM + BN) * 64;
-    static constexpr int kWpe = kTwo ? 2 : BM >= 128 ? 2 : 4;  // waves a SIMD that the registers must allow
-};
 
 // 16 bytes a lane from global memory straight to LDS at `to` + OFF + 16 * lane.  As
 // assembly, because the compiler otherwise waits for the loads in flight to
@@ -413,6 +294,172 @@ __device__ __forceinline__ void unrolled(F f) {
         f(std::integral_constant<int, N - 1>{});
     }
 }
+
+// This wave's loads to LDS but the newest N have landed / its reads of LDS are done.
+template <int N>
+__device__ __forceinline__ void own_loads() {
+    static_assert(N < 64, "the counter has 6 bits");
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+__device__ __forceinline__ void own_reads() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+
+// Streams of a wave: NF tiles of 16 weight rows times MF tiles of 16 rows, steps
+// of 128 bytes through a ring of D steps in LDS that belongs to the wave alone.
+// The way through LDS is for the loads' sake: lanes side by side then cover a
+// row's whole line, where the matrix cores' layout has them on 16 rows, four
+// times the lines for the address unit (17 against 50 bytes a clock and CU, data
+// in L2).  Chunk c of a row sits at c ^ row % 8.
+constexpr int kStreamStep = 128;
+template <int NF, int MF> constexpr int stream_slot() { return 2 * (NF + MF) * 1024; }
+// ring steps of NW waves in KB of LDS, 2 to 4
+template <int NW, int NF, int MF> constexpr int stream_depth(int kb) {
+    const int d = kb * 1024 / (NW * stream_slot<NF, MF>());
+    return d < 2 ? 2 : d > 4 ? 4 : d;
+}
+
+// The place of this lane in a load: row lane / 8 (and 8 more in the second load of
+// a tile), 16-byte chunk stream_chunk() of the step.
+__device__ __forceinline__ int stream_row() { return static_cast<int>(threadIdx.x) % kWave / 8; }
+__device__ __forceinline__ int stream_chunk() { return static_cast<int>(threadIdx.x) % 8 ^ stream_row(); }
+
+// rows[2 t], rows[2 t + 1]: this lane's rows of tile t (the weights' tiles first),
+// at byte 0 of the contraction.
+template <typename T, int NF, int MF, int D>
+__device__ __forceinline__ void stream_products(const char *const (&rows)[2 * (NF + MF)], int s0, int s1, int64_t pitch,
+                                                const char *ring, floatx4 (&acc)[NF][MF]) {
+    constexpr int L = 2 * (NF + MF);
+    const int lane = threadIdx.x % kWave, r = lane % 16, g = lane / 16;
+    const uint32_t at = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) const char *)(ring)));
+    const char *zero = reinterpret_cast<const char *>(kZeroChunk);
+    auto load = [&](int step, int slot) {  // zeros past the run and past the row
+        const int64_t off = static_cast<int64_t>(step) * kStreamStep + stream_chunk() * 16;
+        const bool in = step < s1 && off < pitch;
+        unrolled<L>([&](auto i) {
+            constexpr int k = decltype(i)::value;
+            load_to_lds<k * 1024>(in ? rows[k] + off : zero, at + slot * (L * 1024));
+        });
+    };
+#pragma unroll
+    for (int d = 0; d < D; ++d) load(s0 + d, d);
+    int slot = 0;
+    for (int s = s0; s < s1; ++s) {
+        own_loads<(D - 1) * L>();
+        u32x4 wv[2][NF], xv[2][MF];
+        const char *from = ring + slot * (L * 1024) + r * kStreamStep;
+#pragma unroll
+        for (int kk = 0; kk < 2; ++kk) {
+            const int chunk = ((kk * 4 + g) ^ (r & 7)) * 16;
+#pragma unroll
+            for (int i = 0; i < NF; ++i) wv[kk][i] = *reinterpret_cast<const u32x4 *>(from + i * 2048 + chunk);
+#pragma unroll
+            for (int f = 0; f < MF; ++f) xv[kk][f] = *reinterpret_cast<const u32x4 *>(from + (NF + f) * 2048 + chunk);
+        }
+        own_reads();
+        load(s + D, slot);
+        slot = slot + 1 == D ? 0 : slot + 1;
+#pragma unroll
+        for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+            for (int i = 0; i < NF; ++i)
+#pragma unroll
+                for (int f = 0; f < MF; ++f) acc[i][f] = chunk_mma<T>(wv[kk][i], xv[kk][f], acc[i][f]);
+    }
+    own_loads<0>();
+}
+
+// ------------------------------------------------------------- few rows
+// Groups of a few rows: the time is that of reading the weights.  A workgroup
+// takes MF * 16 rows of a group and NF tiles of 16 weight rows (gated: the value's
+// and the gate's of 16 outputs); its NW waves split the contraction, stream it, and
+// add up through LDS in wave order.
+template <typename T, typename OT, int NW, int NF, int MF, bool GATED, bool ADAPT>
+__global__ void __launch_bounds__(NW * kWave)
+k_rows_few(RowsArgs a, int slices) {
+    static_assert(!GATED || NF == 2, "value and gate");
+    constexpr int BM = MF * 16, kOuts = GATED ? 16 : NF * 16, kTiles = MF * (GATED ? 1 : NF);
+    constexpr int D = stream_depth<NW, NF, MF>(ADAPT ? 160 : 80), kRing = D * stream_slot<NF, MF>();
+    constexpr int kSums = NF * MF * 1024;  // a wave's, in fp32
+    __shared__ __attribute__((aligned(1024))) char lds[NW * (kRing > kSums ? kRing : kSums)];
+    const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const int r = lane % 16, g = lane / 16;
+    RowTile t;
+    if (!find_tile<BM>(a.starts, a.groups, a.rows, block_xy(), slices, t)) return;
+    const int n0 = t.slice * kOuts;
+    int row_id = -1;
+    if constexpr (ADAPT) row_id = adapter_of(a, t.row0 + lane, lane < BM && t.row0 + lane < t.end);
+    const char *rows[2 * (NF + MF)];
+#pragma unroll
+    for (int i = 0; i < 2 * NF; ++i) {
+        const int n = n0 + (GATED ? 0 : i / 2 * 16) + i % 2 * 8 + stream_row();
+        rows[i] = (GATED && i >= 2 ? a.w2 : a.w) +
+                  (static_cast<int64_t>(t.group) * a.c_out + (n < a.c_out ? n : a.c_out - 1)) * a.pitch;
+    }
+#pragma unroll
+    for (int f = 0; f < 2 * MF; ++f) {  // past the end the last row again: its lines are there
+        const int64_t p = t.row0 + f * 8 + stream_row();
+        const int64_t from = source_row(a, p < t.end ? p : t.end - 1);
+        rows[2 * NF + f] = a.x + (from < 0 ? 0 : from) * a.pitch;
+    }
+    floatx4 acc[NF][MF];
+#pragma unroll
+    for (int i = 0; i < NF; ++i)
+#pragma unroll
+        for (int f = 0; f < MF; ++f) acc[i][f] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+    const int steps = static_cast<int>((a.pitch + kStreamStep - 1) / kStreamStep);
+    stream_products<T, NF, MF, D>(rows, steps * wave / NW, steps * (wave + 1) / NW, a.pitch, lds + wave * kRing, acc);
+    if constexpr (ADAPT) add_adapters<T, MF>(a, row_id, t.row0, n0, wave, NW, acc);
+    __syncthreads();  // the rings are done with
+    floatx4 *part = reinterpret_cast<floatx4 *>(lds);  // [wave][i][f][lane]
+#pragma unroll
+    for (int i = 0; i < NF; ++i)
+#pragma unroll
+        for (int f = 0; f < MF; ++f) part[((wave * NF + i) * MF + f) * kWave + lane] = acc[i][f];
+    __syncthreads();
+    // a wave for each tile: the rows f * 16 .. f * 16 + 15 of the outputs' tile i
+    for (int k = wave; k < kTiles; k += NW) {
+        const int f = k % MF, tile = k / MF;
+        const int nn = n0 + tile * 16 + 4 * g;
+        const int64_t p = t.row0 + f * 16 + r;
+        if (nn >= a.c_out || p >= t.end || source_row(a, p) < 0) continue;
+        const int64_t to = target_row(a, p);
+        if (to < 0) continue;
+        floatx4 sum = part[(tile * MF + f) * kWave + lane], sum2 = part[((NF - 1) * MF + f) * kWave + lane];
+#pragma unroll
+        for (int w = 1; w < NW; ++w) {
+            sum += part[((w * NF + tile) * MF + f) * kWave + lane];
+            if (GATED) sum2 += part[((w * NF + NF - 1) * MF + f) * kWave + lane];
+        }
+        float out[4];
+        finish4<GATED>(a, t.group, nn, sum, sum2, out);
+        store_out<OT>(reinterpret_cast<OT *>(a.y) + to * a.c_out + nn, out);
+    }
+}
+
+// ------------------------------------------------------------- many rows
+// Tiles of BM rows x BN outputs through LDS, 64 bytes of the contraction a
+// step, five steps of LDS: the loads run four steps ahead of the products.  A row's 4 chunks are stored at chunk ^ (row / 2 % 4),
+// so 8 neighbouring rows at one chunk cover all banks; the loads go straight to
+// LDS, which fixes a lane's place there, so the swizzle is applied to the
+// address that each lane loads.  Gated: the outputs of a tile are 16 of the
+// value's and 16 of the gate's in turn, so a wave holds both.
+//
+// Tiles of 8 waves run as two groups of four (one wave a SIMD each), half a
+// step apart: while one group multiplies, the other reads its operands from
+// LDS.  Smaller tiles leave that to the several workgroups of a CU.
+
+template <int BM, int BN>
+struct TileCfg {
+    static constexpr int kWavesM = 2, kWavesN = BN >= 256 ? 4 : 2;
+    static constexpr int kWaves = kWavesM * kWavesN;
+    static constexpr int kThreads = kWaves * kWave;
+    static constexpr bool kTwo = kWaves == 8;
+    static constexpr int kMF = BM / kWavesM / 16, kNF = BN / kWavesN / 16;
+    static constexpr int kLoadsX = BM / 16 / kWaves, kLoadsW = BN / 16 / kWaves;  // of 16 rows, per wave and step
+    static constexpr int kLoads = kLoadsX + kLoadsW;
+    static constexpr int kSlots = 5, kAhead = kSlots - 1;  // steps in LDS, steps that the loads run ahead
+    static constexpr int kSlot = (BM + BN) * 64;
+    static constexpr int kWpe = kTwo ? 2 : BM >= 128 ? 2 : 4;  // waves a SIMD that the registers must allow
+};
 
 // All but the newest N of this wave's loads have landed, and its reads of LDS
 // are done; then the barrier.
@@ -676,14 +723,21 @@ k_combine(const float *__restrict__ o, const int32_t *__restrict__ expert, const
     float sum[8];
 #pragma unroll
     for (int u = 0; u < 8; ++u) sum[u] = 0.0f;
-    for (int s = 0; s < top_k; ++s) {
-        const int e = expert[t * top_k + s];
-        if (e < 0 || e >= experts) continue;
-        const float w = weight[t * top_k + s];
-        float v[8];
-        io<float>::load8(o + (t * top_k + s) * C + c, v);
+    for (int s0 = 0; s0 < top_k; s0 += 4) {
+        float v[4][8], w[4];
+        int e[4];
 #pragma unroll
-        for (int u = 0; u < 8; ++u) sum[u] = __builtin_fmaf(w, v[u], sum[u]);
+        for (int j = 0; j < 4; ++j) {  // past the last slot: the last again, not counted
+            const int64_t at = t * top_k + (s0 + j < top_k ? s0 + j : top_k - 1);
+            e[j] = s0 + j < top_k ? expert[at] : -1;
+            w[j] = weight[at];
+            io<float>::load8(o + at * C + c, v[j]);
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int u = 0; u < 8; ++u)
+                sum[u] = e[j] >= 0 && e[j] < experts ? __builtin_fmaf(w[j], v[j][u], sum[u]) : sum[u];
     }
     if (x) {
         float v[8];
@@ -697,90 +751,66 @@ k_combine(const float *__restrict__ o, const int32_t *__restrict__ expert, const
 
 // ------------------------------------------------ an adapter's first half
 // v[row] = scale * A_id x[row], rounded to the storage type (the matrix cores
-// take the second product's operand in it), for 16 rows a workgroup: one
-// distinct adapter of the rows at a time, every gridDim.y-th from blockIdx.y;
-// the waves split the contraction.
-constexpr int kDownWaves = 8;
-
-template <typename T, int NF>
-__global__ void __launch_bounds__(kDownWaves * kWave)
+// take the second product's operand in it), for MF * 16 rows a workgroup: one
+// distinct adapter of the rows at a time, every gridDim.y-th from blockIdx.y.
+// The NW waves split the contraction, stream it, and add up through LDS in wave
+// order.
+template <typename T, int NW, int NF, int MF>
+__global__ void __launch_bounds__(NW * kWave)
 k_adapter_down(const char *__restrict__ x, int64_t rows, int64_t pitch, const char *__restrict__ down,
                const int32_t *__restrict__ ids, const int32_t *__restrict__ ranks, const float *__restrict__ scales,
-               int adapters, int max_rank, char *__restrict__ v, int v_pitch) {
-    __shared__ floatx4 part[kDownWaves - 1][NF][kWave];
-    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+               int adapters, int id_bits, int max_rank, char *__restrict__ v, int v_pitch) {
+    constexpr int D = stream_depth<NW, NF, MF>(160), kRing = D * stream_slot<NF, MF>(), kSums = NF * MF * 1024;
+    __shared__ __attribute__((aligned(1024))) char lds[NW * (kRing > kSums ? kRing : kSums)];
+    floatx4 *part = reinterpret_cast<floatx4 *>(lds);  // [wave][i][f][lane]
+    const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const int r = lane % 16, g = lane / 16;
-    const int64_t row = static_cast<int64_t>(blockIdx.x) * 16 + r;
-    int id = row < rows ? ids[row] : -1;
-    if (id >= adapters) id = -1;
-    const char *xp = x + (row < rows ? row : rows - 1) * pitch;
-    const int64_t steps = (pitch + 63) / 64;
-    const int64_t s0 = steps * wave / kDownWaves, s1 = steps * (wave + 1) / kDownWaves;
-    bool open = id >= 0;
-    for (int turn = 0;; ++turn) {
-        const uint64_t left = __ballot(open);
-        if (!left) break;
-        const int ad = __builtin_amdgcn_readlane(id, __ffsll(static_cast<unsigned long long>(left)) - 1);
-        open = open && id != ad;
-        if (turn % static_cast<int>(gridDim.y) != static_cast<int>(blockIdx.y)) continue;
+    const int64_t row0 = static_cast<int64_t>(blockIdx.x) * (MF * 16);
+    int row_id = lane < MF * 16 && row0 + lane < rows ? ids[row0 + lane] : -1;
+    row_id = row_id >= 0 && row_id < adapters ? row_id : -1;
+    const char *from[2 * (NF + MF)];
+#pragma unroll
+    for (int f = 0; f < 2 * MF; ++f) {
+        const int64_t row = row0 + f * 8 + stream_row();
+        from[2 * NF + f] = x + (row < rows ? row : rows - 1) * pitch;
+    }
+    const int steps = static_cast<int>((pitch + kStreamStep - 1) / kStreamStep);
+    uint64_t left = drop_lanes(distinct_lanes(row_id, id_bits), static_cast<int>(blockIdx.y));
+    while (left) {
+        const int ad = __builtin_amdgcn_readlane(row_id, __ffsll(static_cast<unsigned long long>(left)) - 1);
+        left = drop_lanes(left, static_cast<int>(gridDim.y));
         int rank = ranks ? ranks[ad] : max_rank;
         rank = rank < max_rank ? rank : max_rank;
         const float scale = scales ? scales[ad] : 1.0f;
         const char *base = down + static_cast<int64_t>(ad) * max_rank * pitch;
         for (int n0 = 0; n0 < rank; n0 += NF * 16) {
-            const char *wp[NF];
 #pragma unroll
-            for (int i = 0; i < NF; ++i) {
-                const int n = n0 + i * 16 + r;
-                wp[i] = base + static_cast<int64_t>(n < rank ? n : rank - 1) * pitch;
+            for (int i = 0; i < 2 * NF; ++i) {
+                const int n = n0 + i * 8 + stream_row();
+                from[i] = base + static_cast<int64_t>(n < rank ? n : rank - 1) * pitch;
             }
-            floatx4 acc[NF];
+            floatx4 acc[NF][MF];
 #pragma unroll
-            for (int i = 0; i < NF; ++i) acc[i] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
-            constexpr int U = 4;
-            int64_t s = s0;
-            for (; s + U <= s1 && (s + U) * 64 <= pitch; s += U) {
-                u32x4 wv[U][NF], xv[U];
-                const int64_t off = s * 64 + g * 16;
+            for (int i = 0; i < NF; ++i)
 #pragma unroll
-                for (int u = 0; u < U; ++u) {
-                    xv[u] = *reinterpret_cast<const u32x4 *>(xp + off + u * 64);
+                for (int f = 0; f < MF; ++f) acc[i][f] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+            stream_products<T, NF, MF, D>(from, steps * wave / NW, steps * (wave + 1) / NW, pitch, lds + wave * kRing, acc);
+            __syncthreads();  // the rings are done with
 #pragma unroll
-                    for (int i = 0; i < NF; ++i) wv[u][i] = *reinterpret_cast<const u32x4 *>(wp[i] + off + u * 64);
-                }
+            for (int i = 0; i < NF; ++i)
 #pragma unroll
-                for (int u = 0; u < U; ++u)
-#pragma unroll
-                    for (int i = 0; i < NF; ++i) acc[i] = chunk_mma<T>(wv[u][i], xv[u], acc[i]);
-            }
-            for (; s < s1; ++s) {
-                const int64_t off = s * 64 + g * 16;
-                const bool in = off < pitch;
-                const u32x4 none = {0, 0, 0, 0};
-                const u32x4 xv = in ? *reinterpret_cast<const u32x4 *>(xp + off) : none;
-                u32x4 wv[NF];
-#pragma unroll
-                for (int i = 0; i < NF; ++i) wv[i] = in ? *reinterpret_cast<const u32x4 *>(wp[i] + off) : none;
-#pragma unroll
-                for (int i = 0; i < NF; ++i) acc[i] = chunk_mma<T>(wv[i], xv, acc[i]);
-            }
-            if (wave > 0) {
-#pragma unroll
-                for (int i = 0; i < NF; ++i) part[wave - 1][i][lane] = acc[i];
-            }
+                for (int f = 0; f < MF; ++f) part[((wave * NF + i) * MF + f) * kWave + lane] = acc[i][f];
             __syncthreads();
-            if (wave == 0) {
+            for (int k = wave; k < NF * MF; k += NW) {  // a wave for each tile of the result
+                const int f = k % MF, n = n0 + k / MF * 16 + 4 * g;
+                floatx4 sum = part[k * kWave + lane];
 #pragma unroll
-                for (int i = 0; i < NF; ++i) {
+                for (int w = 1; w < NW; ++w) sum += part[(w * NF * MF + k) * kWave + lane];
+                if (__shfl(row_id, f * 16 + r) == ad && n < max_rank) {
+                    float out[4];
 #pragma unroll
-                    for (int w = 0; w < kDownWaves - 1; ++w) acc[i] += part[w][i][lane];
-                    const int n = n0 + i * 16 + 4 * g;
-                    if (id == ad && n < max_rank) {
-                        float out[4];
-#pragma unroll
-                        for (int u = 0; u < 4; ++u) out[u] = n + u < rank ? scale * acc[i][u] : 0.0f;
-                        io<T>::store4(reinterpret_cast<T *>(v + row * v_pitch) + n, out);
-                    }
+                    for (int u = 0; u < 4; ++u) out[u] = n + u < rank ? scale * sum[u] : 0.0f;
+                    io<T>::store4(reinterpret_cast<T *>(v + (row0 + f * 16 + r) * v_pitch) + n, out);
                 }
             }
             __syncthreads();

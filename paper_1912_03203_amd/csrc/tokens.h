@@ -113,13 +113,15 @@ struct RowsPlan {
     int64_t blocks = 0;
 };
 
-RowsPlan rows_plan(int64_t rows, int64_t groups, bool split, int c_out, bool gated, dynconv_dtype dt) {
+RowsPlan rows_plan(int64_t rows, int64_t groups, bool adapt, int c_out, bool gated, dynconv_dtype dt) {
+    const bool split = !adapt;  // into groups of sizes that only the device knows
     RowsPlan p;
     const int64_t mean = (rows + groups - 1) / groups;
     p.few = mean <= 64;
     if (p.few) {
-        p.bm = mean <= 16 ? 16 : mean <= 32 ? 32 : 64;
-        p.slices = (c_out + 15) / 16;
+        p.bm = static_cast<int>((mean + 15) / 16 * 16);
+        const int outs = gated || adapt ? 16 : 32;
+        p.slices = (c_out + outs - 1) / outs;
     } else {
         const int64_t outs256 = static_cast<int64_t>(c_out) * (gated ? 2 : 1) / 256;
         p.bm = dt != DYNCONV_F32 && mean >= 256 && rows / 256 * outs256 >= 192 ? 256
@@ -134,11 +136,13 @@ RowsPlan rows_plan(int64_t rows, int64_t groups, bool split, int c_out, bool gat
 template <typename T, typename OT, bool GATED, bool ADAPT>
 void launch_rows(const RowsArgs &a, const RowsPlan &p, hipStream_t st, Marks &mk) {
     const dim3 grid = grid_xy(p.blocks);
-    constexpr int NW = 4;
     if (p.few) {
-        if (p.bm == 16) launch(mk, k_rows_few<T, OT, NW, 1, GATED, ADAPT>, grid, dim3(NW * kWave), 0, st, a, p.slices);
-        else if (p.bm == 32) launch(mk, k_rows_few<T, OT, NW, 2, GATED, ADAPT>, grid, dim3(NW * kWave), 0, st, a, p.slices);
-        else launch(mk, k_rows_few<T, OT, NW, 4, GATED, ADAPT>, grid, dim3(NW * kWave), 0, st, a, p.slices);
+        constexpr int NW = ADAPT ? 8 : 4, NF = ADAPT ? 1 : 2;
+        auto go = [&](auto kern) { launch(mk, kern, grid, dim3(NW * kWave), 0, st, a, p.slices); };
+        if (p.bm == 16) go(k_rows_few<T, OT, NW, NF, 1, GATED, ADAPT>);
+        else if (p.bm == 32) go(k_rows_few<T, OT, NW, NF, 2, GATED, ADAPT>);
+        else if (p.bm == 48) go(k_rows_few<T, OT, NW, NF, 3, GATED, ADAPT>);
+        else go(k_rows_few<T, OT, NW, NF, 4, GATED, ADAPT>);
         return;
     }
     if constexpr (sizeof(T) == 2) {
@@ -229,18 +233,27 @@ size_t adapter_bytes(const dynconv_adapters *a, int64_t rows, dynconv_dtype dt) 
 template <typename T>
 void launch_adapters(const RowsArgs &args, const RowsPlan &p, const dynconv_linear *l, const dynconv_adapters *ad,
                      void *v, hipStream_t st, Marks &mk) {
-    // distinct adapters of 16 rows taken at once: all of them where rows are few
-    const int64_t tiles = (args.rows + 15) / 16;
-    const unsigned turns = static_cast<unsigned>(tiles >= 256 ? 1 : std::min<int64_t>({16, args.rows, ad->adapters}));
+    // 32 rows a workgroup where that leaves one for every CU (an adapter's rows
+    // are then read half as often), else 16, with a workgroup for each distinct
+    // adapter that 16 rows can have
+    const bool wide = args.rows >= 32 * 128;
+    const int64_t tiles = (args.rows + (wide ? 31 : 15)) / (wide ? 32 : 16);
+    const unsigned turns = static_cast<unsigned>(tiles >= 256 || wide ? 1 : std::min<int64_t>({16, args.rows, ad->adapters}));
     const dim3 grid(static_cast<unsigned>(tiles), turns);
-    auto go = [&](auto kern) {
-        launch(mk, kern, grid, dim3(kDownWaves * kWave), 0, st, args.x, args.rows, args.pitch,
-               static_cast<const char *>(ad->down), args.ids, ad->ranks, ad->scales, ad->adapters, ad->max_rank,
-               static_cast<char *>(v), args.v_pitch);
+    auto go = [&](auto kern, int waves) {
+        launch(mk, kern, grid, dim3(waves * kWave), 0, st, args.x, args.rows, args.pitch,
+               static_cast<const char *>(ad->down), args.ids, ad->ranks, ad->scales, ad->adapters, args.id_bits,
+               ad->max_rank, static_cast<char *>(v), args.v_pitch);
     };
-    if (ad->max_rank <= 16) go(k_adapter_down<T, 1>);
-    else if (ad->max_rank <= 32) go(k_adapter_down<T, 2>);
-    else go(k_adapter_down<T, 4>);
+    if (wide) {
+        if (ad->max_rank <= 16) go(k_adapter_down<T, 8, 1, 2>, 8);
+        else if (ad->max_rank <= 32) go(k_adapter_down<T, 8, 2, 2>, 8);
+        else go(k_adapter_down<T, 4, 4, 2>, 4);
+    } else {
+        if (ad->max_rank <= 16) go(k_adapter_down<T, 8, 1, 1>, 8);
+        else if (ad->max_rank <= 32) go(k_adapter_down<T, 8, 2, 1>, 8);
+        else go(k_adapter_down<T, 8, 4, 1>, 8);
+    }
     launch_rows<T, T, false, true>(args, p, st, mk);
 }
 
@@ -315,7 +328,7 @@ dynconv_status dynconv_grouped_linear(const void *x, int64_t x_rows, void *y, in
     a.y = static_cast<char *>(y);
     a.y_rows = y_rows;
     a.dst = dst;
-    const RowsPlan p = rows_plan(rows, groups, true, l->c_out, false, dt);
+    const RowsPlan p = rows_plan(rows, groups, false, l->c_out, false, dt);
     if (p.blocks > kMaxTokenRows) return DYNCONV_ERR_UNSUPPORTED;
     (void)hipGetLastError();
     Marks mk;
@@ -365,7 +378,7 @@ dynconv_status dynconv_experts_forward(const void *x, void *y, int64_t tokens, d
     a.y = static_cast<char *>(ws);
     a.y_rows = rows;
     const bool gated = e->w_gate != nullptr;
-    const RowsPlan p1 = rows_plan(rows, e->experts, true, e->c_hidden, gated, dt);
+    const RowsPlan p1 = rows_plan(rows, e->experts, false, e->c_hidden, gated, dt);
     RowsArgs o = a;
     o.x = static_cast<const char *>(ws);
     o.x_rows = rows;
@@ -380,7 +393,7 @@ dynconv_status dynconv_experts_forward(const void *x, void *y, int64_t tokens, d
     o.act = DYNCONV_ACT_NONE;
     o.y = at(ws, L.out);
     o.dst = routes->rows;
-    const RowsPlan p2 = rows_plan(rows, e->experts, true, e->c_out, false, dt);
+    const RowsPlan p2 = rows_plan(rows, e->experts, false, e->c_out, false, dt);
     if (p1.blocks > kMaxTokenRows || p2.blocks > kMaxTokenRows) return DYNCONV_ERR_UNSUPPORTED;
     hipStream_t st = static_cast<hipStream_t>(stream);
     (void)hipGetLastError();
@@ -434,7 +447,8 @@ dynconv_status dynconv_adapter_linear(const void *x, void *y, int64_t rows, dync
     a.ranks = adapters->ranks;
     a.adapters = adapters->adapters;
     a.max_rank = adapters->max_rank;
-    const RowsPlan p = rows_plan(rows, 1, false, l->c_out, false, dt);
+    a.id_bits = bits_for(adapters->adapters);
+    const RowsPlan p = rows_plan(rows, 1, true, l->c_out, false, dt);
     if (p.blocks > kMaxTokenRows) return DYNCONV_ERR_UNSUPPORTED;
     hipStream_t st = static_cast<hipStream_t>(stream);
     (void)hipGetLastError();
