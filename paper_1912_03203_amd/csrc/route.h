@@ -77,22 +77,26 @@ __device__ __forceinline__ uint32_t order_key(float v) {
 // exp(v - top) where equal infinities count as 1
 __device__ __forceinline__ float exp_below(float v, float top) { return v == top ? 1.0f : expf(v - top); }
 
-// One row on G lanes, V = ceil(E / G) experts a lane (expert v * G + lane).
-// Lane j < top_k returns slot j: expert (-1: none) and weight.
+// A row of logits on G lanes, V = ceil(E / G) experts a lane (expert v * G + lane).
 template <typename T, int G, int V>
-__device__ __forceinline__ void choose_row(const T *__restrict__ row, bool on, int E, int top_k,
+__device__ __forceinline__ void load_row(const T *__restrict__ row, bool on, int E, int lane, float (&l)[V]) {
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        const int e = v * G + lane;
+        l[v] = on && e < E ? static_cast<float>(row[e]) : -__builtin_huge_valf();
+    }
+}
+
+// Chooses for the row in l.  Lane j < top_k returns slot j: expert (-1: none) and
+// weight.
+template <typename T, int G, int V>
+__device__ __forceinline__ void choose_row(const float (&l)[V], const T *__restrict__ row, int E, int top_k,
                                            const float *__restrict__ bias, int flags, float scale, int lane,
                                            int &expert, float &weight) {
     uint32_t key[V];
     float all_top = -__builtin_huge_valf(), all_sum = 0.0f;
     const bool whole = !(flags & (kRouteSigmoid | kRouteRenormalize));  // softmax over every live expert
     {
-        float l[V];
-#pragma unroll
-        for (int v = 0; v < V; ++v) {
-            const int e = v * G + lane;
-            l[v] = on && e < E ? static_cast<float>(row[e]) : -__builtin_huge_valf();
-        }
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             const int e = v * G + lane;
@@ -124,14 +128,14 @@ __device__ __forceinline__ void choose_row(const T *__restrict__ row, bool on, i
         if (lane == j && m != 0) expert = static_cast<int>(at);
     }
     weight = 0.0f;
-    const float l = expert >= 0 ? static_cast<float>(row[expert]) : -__builtin_huge_valf();
+    const float le = expert >= 0 ? static_cast<float>(row[expert]) : -__builtin_huge_valf();
     if (flags & kRouteSigmoid) {
-        const float s = expert >= 0 ? 1.0f / (1.0f + expf(-l)) : 0.0f;
+        const float s = expert >= 0 ? 1.0f / (1.0f + expf(-le)) : 0.0f;
         const float sum = (flags & kRouteRenormalize) ? group_sumf<G>(s) : 1.0f;
         if (s > 0.0f) weight = scale * (s / sum);
     } else {
-        const float top = whole ? all_top : group_maxf<G>(l);
-        const float p = expert >= 0 ? exp_below(l, top) : 0.0f;
+        const float top = whole ? all_top : group_maxf<G>(le);
+        const float p = expert >= 0 ? exp_below(le, top) : 0.0f;
         const float sum = whole ? all_sum : group_sumf<G>(p);
         if (expert >= 0) weight = scale * (p / sum);
     }
@@ -229,16 +233,25 @@ __device__ __forceinline__ void choose_rows(const T *__restrict__ logits, int64_
                                             float scale, int32_t *__restrict__ expert, float *__restrict__ weight,
                                             uint16_t *ids) {
     const int lane = threadIdx.x % G;
-    for (int64_t t = t0 + threadIdx.x / G; t < t1; t += NT / G) {
-        const bool on = !mask || mask[t] != 0;
+    auto fetch = [&](int64_t t, float (&to)[V]) {
+        load_row<T, G, V>(logits + t * E, !mask || mask[t] != 0, E, lane, to);
+    };
+    float l[V], after[V];
+    int64_t t = t0 + threadIdx.x / G;
+    if (t < t1) fetch(t, l);
+    for (; t < t1; t += NT / G) {
+        // the next row comes while this one is chosen from
+        if (t + NT / G < t1) fetch(t + NT / G, after);
         int e;
         float w;
-        choose_row<T, G, V>(logits + t * E, on, E, top_k, bias, flags, scale, lane, e, w);
+        choose_row<T, G, V>(l, logits + t * E, E, top_k, bias, flags, scale, lane, e, w);
         if (lane < top_k) {
             expert[t * top_k + lane] = e;
             weight[t * top_k + lane] = w;
             ids[(t - t0) * top_k + lane] = static_cast<uint16_t>(e < 0 ? E : e);
         }
+#pragma unroll
+        for (int v = 0; v < V; ++v) l[v] = after[v];
     }
 }
 
@@ -280,8 +293,8 @@ k_route_one(const T *__restrict__ logits, int tokens, int E, int top_k, int bits
 // Rows per workgroup of the two-launch form: at most kRouteChunk assignments.
 constexpr int kRouteChunk = 2048;
 
-template <typename T, int G, int V>
-__global__ void __launch_bounds__(kRouteThreads)
+template <typename T, int G, int V, int NT>
+__global__ void __launch_bounds__(NT)
 k_route_choose(const T *__restrict__ logits, int64_t tokens, int per, int E, int top_k, const float *__restrict__ bias,
                const uint8_t *__restrict__ mask, int flags, float scale, int32_t *__restrict__ expert,
                float *__restrict__ weight, int32_t *__restrict__ hist) {
@@ -289,13 +302,13 @@ k_route_choose(const T *__restrict__ logits, int64_t tokens, int per, int E, int
     __shared__ int count[kMaxExperts + 1];
     const int64_t t0 = static_cast<int64_t>(blockIdx.x) * per;
     const int64_t t1 = t0 + per < tokens ? t0 + per : tokens;
-    for (int e = threadIdx.x; e <= E; e += kRouteThreads) count[e] = 0;
-    choose_rows<T, G, V, kRouteThreads>(logits, t0, t1, E, top_k, bias, mask, flags, scale, expert, weight, ids);
+    for (int e = threadIdx.x; e <= E; e += NT) count[e] = 0;
+    choose_rows<T, G, V, NT>(logits, t0, t1, E, top_k, bias, mask, flags, scale, expert, weight, ids);
     __syncthreads();
     const int n = static_cast<int>(t1 - t0) * top_k;
-    for (int i = threadIdx.x; i < n; i += kRouteThreads) atomicAdd(&count[ids[i]], 1);
+    for (int i = threadIdx.x; i < n; i += NT) atomicAdd(&count[ids[i]], 1);
     __syncthreads();
-    for (int e = threadIdx.x; e <= E; e += kRouteThreads)
+    for (int e = threadIdx.x; e <= E; e += NT)
         hist[static_cast<int64_t>(blockIdx.x) * (E + 1) + e] = count[e];
 }
 
@@ -306,18 +319,27 @@ k_route_scan(int32_t *__restrict__ hist, int blocks, int stride, int32_t *__rest
     const int lane = threadIdx.x % kWave;
     const int e = blockIdx.x * kWavesPerBlock + threadIdx.x / kWave;
     if (e >= stride) return;
+    constexpr int kOnce = 4;  // loads in flight
     int run = 0;
-    for (int b0 = 0; b0 < blocks; b0 += kWave) {
-        const int b = b0 + lane;
-        const int c = b < blocks ? hist[static_cast<int64_t>(b) * stride + e] : 0;
-        int incl = c;
+    for (int b0 = 0; b0 < blocks; b0 += kOnce * kWave) {
+        int c[kOnce];
 #pragma unroll
-        for (int d = 1; d < kWave; d <<= 1) {
-            const int o = __shfl_up(incl, d);
-            if (lane >= d) incl += o;
+        for (int i = 0; i < kOnce; ++i) {
+            const int b = b0 + i * kWave + lane;
+            c[i] = b < blocks ? hist[static_cast<int64_t>(b) * stride + e] : 0;
         }
-        if (b < blocks) hist[static_cast<int64_t>(b) * stride + e] = run + incl - c;
-        run += __shfl(incl, kWave - 1);
+#pragma unroll
+        for (int i = 0; i < kOnce; ++i) {
+            const int b = b0 + i * kWave + lane;
+            int incl = c[i];
+#pragma unroll
+            for (int d = 1; d < kWave; d <<= 1) {
+                const int o = __shfl_up(incl, d);
+                if (lane >= d) incl += o;
+            }
+            if (b < blocks) hist[static_cast<int64_t>(b) * stride + e] = run + incl - c[i];
+            run += __shfl(incl, kWave - 1);
+        }
     }
     if (lane == 0) totals[e] = run;
 }
