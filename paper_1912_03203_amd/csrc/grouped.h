@@ -749,6 +749,64 @@ k_combine(const float *__restrict__ o, const int32_t *__restrict__ expert, const
     io<T>::store4(y + t * C + c + 4, sum + 4);
 }
 
+// --------------------------------------------- the second product of few tokens
+// y[t] = (x[t]) + sum over slots of weight * (W_e h[t * k + slot] + b_e), e the
+// slot's expert, in one launch: for calls of so few tokens that hardly two take
+// the same expert, so that nothing is lost by reading the weights for each.  A
+// workgroup takes one token and 16 outputs; a wave takes every NW-th slot and
+// streams its expert's rows, or with fewer slots than waves several waves a part of
+// the contraction each.  Slots and parts are added in their order, in fp32.
+template <typename T, int NW>
+__global__ void __launch_bounds__(NW * kWave)
+k_project_tokens(const char *__restrict__ h, int64_t pitch, const int32_t *__restrict__ expert,
+                 const float *__restrict__ weight, int top_k, int experts, const char *__restrict__ w,
+                 const float *__restrict__ b, const T *x, T *y, int c_out, int slices) {
+    constexpr int D = stream_depth<NW, 1, 1>(160), kRing = D * stream_slot<1, 1>();
+    __shared__ __attribute__((aligned(1024))) char lds[NW * kRing];
+    __shared__ floatx4 part[kMaxTopK > NW ? kMaxTopK : NW][4];  // [slot][part of the contraction][16 outputs]
+    const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const int64_t t = blockIdx.x / static_cast<unsigned>(slices);
+    const int n0 = static_cast<int>(blockIdx.x % static_cast<unsigned>(slices)) * 16;
+    const int steps = static_cast<int>((pitch + kStreamStep - 1) / kStreamStep);
+    const int parts = top_k < NW ? NW / top_k : 1, mine = wave % parts;
+    for (int s = wave / parts; s < top_k; s += NW) {
+        const int e = __builtin_amdgcn_readfirstlane(expert[t * top_k + s]);
+        if (e < 0 || e >= experts) continue;
+        const char *rows[4];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int n = n0 + i * 8 + stream_row();
+            rows[i] = w + (static_cast<int64_t>(e) * c_out + (n < c_out ? n : c_out - 1)) * pitch;
+            rows[2 + i] = h + (t * top_k + s) * pitch;  // one row: every lane's
+        }
+        floatx4 acc[1][1] = {{floatx4{0.0f, 0.0f, 0.0f, 0.0f}}};
+        stream_products<T, 1, 1, D>(rows, steps * mine / parts, steps * (mine + 1) / parts, pitch, lds + wave * kRing, acc);
+        if (lane % 16 == 0) part[s * parts + mine][lane / 16] = acc[0][0];
+    }
+    __syncthreads();
+    const int n = n0 + 4 * static_cast<int>(threadIdx.x);
+    if (threadIdx.x >= 4 || n >= c_out) return;
+    float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int s = 0; s < top_k; ++s) {
+        const int e = expert[t * top_k + s];
+        if (e < 0 || e >= experts) continue;
+        const float k = weight[t * top_k + s];
+        float bias[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        if (b) io<float>::load4(b + static_cast<int64_t>(e) * c_out + n, bias);
+        floatx4 v = part[s * parts][threadIdx.x];
+        for (int i = 1; i < parts; ++i) v += part[s * parts + i][threadIdx.x];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) sum[u] = __builtin_fmaf(k, v[u] + bias[u], sum[u]);
+    }
+    if (x) {
+        float v[4];
+        io<T>::load4(x + t * c_out + n, v);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) sum[u] += v[u];
+    }
+    io<T>::store4(y + t * c_out + n, sum);
+}
+
 // ------------------------------------------------ an adapter's first half
 // v[row] = scale * A_id x[row], rounded to the storage type (the matrix cores
 // take the second product's operand in it), for MF * 16 rows a workgroup: one

@@ -215,6 +215,21 @@ void launch_combine(const float *o, const dynconv_routes *r, const void *x, void
            static_cast<const T *>(x), static_cast<T *>(y), tokens, C, top_k, experts);
 }
 
+// Few tokens: one launch for the second product and the sum.  A token's experts
+// differ, so one token always gains; more do while their choices seldom meet.
+bool few_tokens(int64_t tokens, int top_k, int experts) {
+    return tokens == 1 || tokens * top_k * 2 <= experts;
+}
+
+template <typename T>
+void launch_project_tokens(const RowsArgs &o, const dynconv_routes *r, const void *x, void *y, int64_t tokens, int top_k,
+                           int experts, hipStream_t st, Marks &mk) {
+    constexpr int NW = 8;
+    const int slices = (o.c_out + 15) / 16;
+    launch(mk, k_project_tokens<T, NW>, dim3(static_cast<unsigned>(tokens * slices)), dim3(NW * kWave), 0, st, o.x, o.pitch,
+           r->expert, r->weight, top_k, experts, o.w, o.b, static_cast<const T *>(x), static_cast<T *>(y), o.c_out, slices);
+}
+
 // ------------------------------------------------------------- adapters
 dynconv_status check_adapters(const dynconv_linear *l, const dynconv_adapters *a, int64_t rows, dynconv_dtype dt) {
     if (!l || !a) return DYNCONV_ERR_NULL;
@@ -383,6 +398,8 @@ dynconv_status dynconv_experts_forward(const void *x, void *y, int64_t tokens, d
     a.act = e->act;
     a.y = static_cast<char *>(ws);
     a.y_rows = rows;
+    const bool few = few_tokens(tokens, top_k, e->experts);
+    if (few) a.dst = routes->rows;  // hidden rows at their assignments, not in list order
     const bool gated = e->w_gate != nullptr;
     const RowsPlan p1 = rows_plan(rows, e->experts, false, e->c_hidden, gated, dt);
     RowsArgs o = a;
@@ -404,9 +421,16 @@ dynconv_status dynconv_experts_forward(const void *x, void *y, int64_t tokens, d
     hipStream_t st = static_cast<hipStream_t>(stream);
     (void)hipGetLastError();
     Marks mk;
-    dispatch_rows(dt, a, p1, gated, false, st, mk);
-    dispatch_rows(dt, o, p2, false, true, st, mk);
     const void *res = (flags & DYNCONV_EXPERTS_RESIDUAL) ? x : nullptr;
+    dispatch_rows(dt, a, p1, gated, false, st, mk);
+    if (few) {
+        auto go = [&](auto f) { f(o, routes, res, y, tokens, top_k, e->experts, st, mk); };
+        if (dt == DYNCONV_F32) go(launch_project_tokens<float>);
+        else if (dt == DYNCONV_F16) go(launch_project_tokens<half_t>);
+        else go(launch_project_tokens<bf16_t>);
+        return launch_status();
+    }
+    dispatch_rows(dt, o, p2, false, true, st, mk);
     const float *oo = at<const float>(ws, L.out);
     auto go = [&](auto f) { f(oo, routes, res, y, tokens, e->c_out, top_k, e->experts, st, mk); };
     if (dt == DYNCONV_F32) go(launch_combine<float>);

@@ -251,7 +251,10 @@ def device_weights(weights):
 @pytest.mark.parametrize("tokens,experts,top_k,c_in,hidden,c_out,gated,biases,residual", [
     (1, 8, 2, 64, 48, 64, True, False, True), (5, 4, 4, 40, 24, 72, False, True, False),
     (33, 6, 2, 136, 72, 136, True, True, True), (120, 3, 2, 96, 104, 96, True, False, False),
-    (200, 2, 1, 48, 136, 48, False, False, True), (260, 3, 3, 72, 264, 200, True, True, False)])
+    (200, 2, 1, 48, 136, 48, False, False, True), (260, 3, 3, 72, 264, 200, True, True, False),
+    # few tokens, whose experts seldom meet: more slots than waves, masked tokens, one expert
+    (1, 40, 16, 200, 88, 72, False, True, False), (10, 96, 4, 72, 264, 72, True, True, True),
+    (3, 64, 10, 136, 40, 136, True, False, True), (1, 1, 1, 8, 8, 8, True, True, True)])
 def test_experts(dtype, tokens, experts, top_k, c_in, hidden, c_out, gated, biases, residual):
     kind = dc.ACT_SILU if gated else dc.ACT_GELU
     x, weights, logits, mask = expert_case((tokens, experts), tokens, experts, top_k, c_in, hidden, c_out, dtype, gated,
