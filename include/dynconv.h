@@ -553,8 +553,8 @@ typedef struct {
  * each expert, and dst = rows puts results back at their assignments.
  *   x      (device) [x_rows][c_in];  y (device) [y_rows][c_out], not
  *          overlapping x; rows that no position names stay as they are
- *   starts (device) int32 [groups + 1], ascending, groups <= 1024; values are
- *          taken as if cut to 0 .. rows
+ *   starts (device) int32 [groups + 1], groups <= 1024, ascending (if they are
+ *          not, nothing is computed); values are taken as if cut to 0 .. rows
  *   rows   list positions; src and dst (device) int32 [rows] or NULL (then
  *          x_rows or y_rows must be at least rows); the entries of dst are
  *          distinct; src_div >= 1, 1 without src
@@ -605,8 +605,9 @@ dynconv_status dynconv_experts_forward(const void *x, void *y, int64_t tokens, d
  *   down [adapters][max_rank][c_in], up [adapters][c_out][max_rank] in the
  *   storage dtype, max_rank a multiple of 8 up to 256; ranks int32 [adapters]
  *   or NULL (all max_rank): rows of down from ranks[i] on are not read, columns
- *   of up from ranks[i] on do not count but have to be finite; scales fp32
- *   [adapters] or NULL (1)
+ *   of up from ranks[i] on do not count; scales fp32 [adapters] or NULL (1).
+ *   up has to be finite throughout: rows without an adapter are multiplied with
+ *   it as zeros, so that an infinity or NaN in it could reach rows beside its own
  */
 typedef struct {
     int32_t adapters, max_rank;

@@ -92,13 +92,17 @@ __device__ __forceinline__ int64_t clamp_row(int64_t v, int64_t rows) { return v
 
 constexpr int kBand = 8;
 
+// Tiles of group g and its rows; ascends: whether its end is not before its start.
 template <int BM>
 __device__ __forceinline__ int group_tiles(const int32_t *__restrict__ starts, int groups, int64_t rows, int g, int &lo,
-                                           int &hi) {
+                                           int &hi, bool &ascends) {
     lo = hi = 0;
+    ascends = true;
     if (g < groups) {
-        lo = static_cast<int>(clamp_row(starts[g], rows));
-        hi = static_cast<int>(clamp_row(starts[g + 1], rows));
+        const int s = starts[g], e = starts[g + 1];
+        ascends = s <= e;
+        lo = static_cast<int>(clamp_row(s, rows));
+        hi = static_cast<int>(clamp_row(e, rows));
     }
     return hi > lo ? static_cast<int>((static_cast<int64_t>(hi) - lo + BM - 1) / BM) : 0;
 }
@@ -123,7 +127,10 @@ __device__ __forceinline__ bool find_tile(const int32_t *__restrict__ starts, in
     } else {
         int sum = 0;
         for (int g0 = 0; g0 < groups; g0 += kWave) {
-            n = group_tiles<BM>(starts, groups, rows, g0 + lane, lo, hi);
+            bool ascends;
+            n = group_tiles<BM>(starts, groups, rows, g0 + lane, lo, hi, ascends);
+            // starts that do not ascend could name more tiles than a launch counts
+            if (__ballot(!ascends)) return false;
             incl = wave_incl(n, lane);
             sum += __builtin_amdgcn_readlane(incl, kWave - 1);
         }
@@ -147,7 +154,8 @@ __device__ __forceinline__ bool find_tile(const int32_t *__restrict__ starts, in
     int before = 0;
     for (int g0 = 0; g0 < groups; g0 += kWave) {
         if (groups > kWave) {
-            n = group_tiles<BM>(starts, groups, rows, g0 + lane, lo, hi);
+            bool ascends;
+            n = group_tiles<BM>(starts, groups, rows, g0 + lane, lo, hi, ascends);
             incl = wave_incl(n, lane);
         }
         const uint64_t past = __ballot(before + incl > tile);
@@ -282,7 +290,7 @@ template <int OFF>
 __device__ __forceinline__ void load_to_lds(const char *from, uint32_t to) {
     asm volatile("s_add_u32 m0, %0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(DC_UNIFORM(to)), "v"(from),
                  "n"(OFF)
-                 : "scc");
+                 : "scc", "m0");
 }
 #undef DC_UNIFORM
 
@@ -810,7 +818,7 @@ k_project_tokens(const char *__restrict__ h, int64_t pitch, const int32_t *__res
 // ------------------------------------------------ an adapter's first half
 // v[row] = scale * A_id x[row], rounded to the storage type (the matrix cores
 // take the second product's operand in it), for MF * 16 rows a workgroup: one
-// distinct adapter of the rows at a time, every gridDim.y-th from blockIdx.y.
+// distinct adapter of the rows at a time, every gridDim.z-th from blockIdx.z.
 // The NW waves split the contraction, stream it, and add up through LDS in wave
 // order.
 template <typename T, int NW, int NF, int MF>
@@ -823,7 +831,7 @@ k_adapter_down(const char *__restrict__ x, int64_t rows, int64_t pitch, const ch
     floatx4 *part = reinterpret_cast<floatx4 *>(lds);  // [wave][i][f][lane]
     const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const int r = lane % 16, g = lane / 16;
-    const int64_t row0 = static_cast<int64_t>(blockIdx.x) * (MF * 16);
+    const int64_t row0 = static_cast<int64_t>(block_xy()) * (MF * 16);
     int row_id = lane < MF * 16 && row0 + lane < rows ? ids[row0 + lane] : -1;
     row_id = row_id >= 0 && row_id < adapters ? row_id : -1;
     const char *from[2 * (NF + MF)];
@@ -833,10 +841,10 @@ k_adapter_down(const char *__restrict__ x, int64_t rows, int64_t pitch, const ch
         from[2 * NF + f] = x + (row < rows ? row : rows - 1) * pitch;
     }
     const int steps = static_cast<int>((pitch + kStreamStep - 1) / kStreamStep);
-    uint64_t left = drop_lanes(distinct_lanes(row_id, id_bits), static_cast<int>(blockIdx.y));
+    uint64_t left = drop_lanes(distinct_lanes(row_id, id_bits), static_cast<int>(blockIdx.z));
     while (left) {
         const int ad = __builtin_amdgcn_readlane(row_id, __ffsll(static_cast<unsigned long long>(left)) - 1);
-        left = drop_lanes(left, static_cast<int>(gridDim.y));
+        left = drop_lanes(left, static_cast<int>(gridDim.z));
         int rank = ranks ? ranks[ad] : max_rank;
         rank = rank < max_rank ? rank : max_rank;
         const float scale = scales ? scales[ad] : 1.0f;

@@ -260,7 +260,8 @@ void launch_adapters(const RowsArgs &args, const RowsPlan &p, const dynconv_line
     const bool wide = args.rows >= 32 * 128;
     const int64_t tiles = (args.rows + (wide ? 31 : 15)) / (wide ? 32 : 16);
     const unsigned turns = static_cast<unsigned>(tiles >= 256 || wide ? 1 : std::min<int64_t>({16, args.rows, ad->adapters}));
-    const dim3 grid(static_cast<unsigned>(tiles), turns);
+    dim3 grid = grid_xy(tiles);
+    grid.z = turns;
     auto go = [&](auto kern, int waves) {
         launch(mk, kern, grid, dim3(waves * kWave), 0, st, args.x, args.rows, args.pitch,
                static_cast<const char *>(ad->down), args.ids, ad->ranks, ad->scales, ad->adapters, args.id_bits,

@@ -621,9 +621,13 @@ def _storage(x, name):
 
 class _Prepared:
     """A call marshalled once: calling it enqueues it on `stream` (default: the
-    current stream of the tensors' device)."""
+    current stream of the tensors' device).  The object holds its tensors and its
+    workspace, so it has to live until its work is done, and calls of one object
+    must not overlap in time."""
 
     def _prepare(self, device, fn, name, args):
+        if device.type != "cuda":
+            raise DynconvError("%s: the tensors are on %s, not on a GPU" % (name, device))
         self._device, self._fn, self._name, self._cargs = device, fn, name, args
         self._index = device.index if device.index is not None else torch.cuda.current_device()
 

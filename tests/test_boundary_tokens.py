@@ -212,6 +212,9 @@ def test_binding_checks_its_tensors():
     bad("b: shape", x, y, w, torch.zeros(3, 16), starts)
     bad("src and dst", x, y, w, None, starts, src=starts, dst=starts[:2])
     bad("y: on meta", x, y.to("meta"), w, None, starts)
+    bad("not on a GPU", x, y, w, None, starts)
+    with pytest.raises(dc.DynconvError, match="not on a GPU"):
+        dc.Router(torch.zeros(4, 8), 2)
     with pytest.raises(dc.DynconvError, match="mask: dtype"):
         dc.Router(torch.zeros(4, 8), 2, mask=torch.ones(4, dtype=torch.bool))
     with pytest.raises(dc.DynconvError, match="rejected"):

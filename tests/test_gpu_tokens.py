@@ -211,6 +211,26 @@ def test_grouped_skips_what_lists_do_not_name():
             within(got, want, bound, "skip")
 
 
+@pytest.mark.parametrize("rows", [20, 900])
+def test_grouped_refuses_starts_that_do_not_ascend(rows):
+    """Nothing is computed or written, whatever the groups around the fault."""
+    gen = gen_for("descend", rows)
+    x, w = normal(gen, (rows, 64), torch.float16), normal(gen, (70, 32, 64), torch.float16, 0.125)
+    for at in (1, 40, 66):
+        starts = torch.arange(71, dtype=torch.int32) * rows // 70
+        starts[at] = rows + 7 if at < 60 else -2
+        y = torch.full((rows, 32), 3.0, dtype=torch.float16, device=DEV)
+        dc.grouped_linear(dev(x), y, dev(w), None, dev(starts))
+        assert bool((y == 3.0).all())
+
+
+def test_grouped_many_groups():
+    """More groups than a wave looks at in one step, in every form of the products."""
+    for rows, groups in ((300, 130), (2600, 130), (9000, 70)):
+        check_grouped(("many", rows), rows, groups, 40, 24, TYPES[rows % 3], kind=dc.ACT_RELU)
+        check_grouped(("many", rows, 1), rows, groups, 40, 24, TYPES[(rows + 1) % 3], "both", div=2)
+
+
 def test_grouped_keeps_nan_in_its_rows():
     gen = gen_for("nan")
     for rows in (30, 400):
@@ -269,6 +289,20 @@ def test_experts(dtype, tokens, experts, top_k, c_in, hidden, c_out, gated, bias
     torch.cuda.synchronize()
     assert y.intact()
     within(got, want, bound, "experts")
+
+
+@pytest.mark.parametrize("dtype", TYPES[1:])
+def test_experts_large_tiles(dtype):
+    """Enough rows and widths for the largest tiles, gated, with edges on every side."""
+    tokens, top_k = 3301, 2
+    x, weights, logits, mask = expert_case("large", tokens, 2, top_k, 72, 1096, 72, dtype, True, True, dc.ACT_SILU, 0.05)
+    r = dc.route(dev(logits), top_k, mask=dev(mask))
+    some = torch.cat([torch.arange(0, tokens, 97), torch.arange(tokens - 9, tokens)])
+    want, bound = plain.experts(x[some], weights, r.expert.cpu()[some], r.weight.cpu()[some], True)
+    got = dc.experts_forward(dev(x), torch.full((tokens, 72), math.nan, dtype=dtype, device=DEV), device_weights(weights), r,
+                             flags=dc.EXPERTS_RESIDUAL)
+    within(got.cpu()[some], want, bound, "large experts")
+    assert bool(torch.isfinite(got).all())
 
 
 def test_experts_in_place_and_all_rows_masked():
@@ -331,10 +365,11 @@ def test_adapters_in_any_order(order, rows):
     check_adapters((order, rows), rows, 9, 16, 72, 56, TYPES[rows % 3], rows != 60, rows != 20, dc.ACT_SILU, order)
 
 
-def test_adapters_large_tiles():
-    gen = gen_for("adapters large")
-    rows, c_in, c_out, n, rank = 4200, 136, 4104, 5, 24
-    dtype = torch.bfloat16
+@pytest.mark.parametrize("rank,c_out,dtype", [(16, 72, torch.float16), (24, 4104, torch.bfloat16), (128, 136, torch.bfloat16),
+                                              (64, 72, torch.float32)])
+def test_adapters_large_tiles(rank, c_out, dtype):
+    gen = gen_for("adapters large", rank)
+    rows, c_in, n = 4200, 136, 5
     x, w = normal(gen, (rows, c_in), dtype), normal(gen, (c_out, c_in), dtype, c_in ** -0.5)
     down, up = normal(gen, (n, rank, c_in), dtype, c_in ** -0.5), normal(gen, (n, c_out, rank), dtype, rank ** -0.5)
     ids = (torch.arange(rows) // 700 - 1).to(torch.int32)
