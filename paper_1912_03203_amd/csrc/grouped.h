@@ -817,26 +817,29 @@ k_project_tokens(const char *__restrict__ h, int64_t pitch, const int32_t *__res
 
 // ------------------------------------------------ an adapter's first half
 // v[row] = scale * A_id x[row], rounded to the storage type (the matrix cores
-// take the second product's operand in it), for MF * 16 rows a workgroup: one
-// distinct adapter of the rows at a time, every gridDim.z-th from blockIdx.z.
-// The NW waves split the contraction, stream it, and add up through LDS in wave
-// order.
-template <typename T, int NW, int NF, int MF>
-__global__ void __launch_bounds__(NW * kWave)
+// take the second product's operand in it), for 16 rows a workgroup: one distinct
+// adapter of the rows at a time, every gridDim.z-th from blockIdx.z, NF tiles of 16
+// of its rows.  The waves split the contraction, stream it, and add up through LDS
+// in wave order.
+constexpr int kDownWaves = 8;
+
+template <typename T, int NF>
+__global__ void __launch_bounds__(kDownWaves * kWave)
 k_adapter_down(const char *__restrict__ x, int64_t rows, int64_t pitch, const char *__restrict__ down,
                const int32_t *__restrict__ ids, const int32_t *__restrict__ ranks, const float *__restrict__ scales,
                int adapters, int id_bits, int max_rank, char *__restrict__ v, int v_pitch) {
-    constexpr int D = stream_depth<NW, NF, MF>(160), kRing = D * stream_slot<NF, MF>(), kSums = NF * MF * 1024;
-    __shared__ __attribute__((aligned(1024))) char lds[NW * (kRing > kSums ? kRing : kSums)];
-    floatx4 *part = reinterpret_cast<floatx4 *>(lds);  // [wave][i][f][lane]
+    constexpr int NW = kDownWaves, D = stream_depth<NW, NF, 1>(160), kRing = D * stream_slot<NF, 1>();
+    static_assert(kRing >= NF * 1024, "a wave's sums fit its ring");
+    __shared__ __attribute__((aligned(1024))) char lds[NW * kRing];
+    floatx4 *part = reinterpret_cast<floatx4 *>(lds);  // [wave][i][lane]
     const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const int r = lane % 16, g = lane / 16;
-    const int64_t row0 = static_cast<int64_t>(block_xy()) * (MF * 16);
-    int row_id = lane < MF * 16 && row0 + lane < rows ? ids[row0 + lane] : -1;
+    const int64_t row0 = static_cast<int64_t>(block_xy()) * 16;
+    int row_id = lane < 16 && row0 + lane < rows ? ids[row0 + lane] : -1;
     row_id = row_id >= 0 && row_id < adapters ? row_id : -1;
-    const char *from[2 * (NF + MF)];
+    const char *from[2 * (NF + 1)];
 #pragma unroll
-    for (int f = 0; f < 2 * MF; ++f) {
+    for (int f = 0; f < 2; ++f) {
         const int64_t row = row0 + f * 8 + stream_row();
         from[2 * NF + f] = x + (row < rows ? row : rows - 1) * pitch;
     }
@@ -855,28 +858,24 @@ k_adapter_down(const char *__restrict__ x, int64_t rows, int64_t pitch, const ch
                 const int n = n0 + i * 8 + stream_row();
                 from[i] = base + static_cast<int64_t>(n < rank ? n : rank - 1) * pitch;
             }
-            floatx4 acc[NF][MF];
+            floatx4 acc[NF][1];
 #pragma unroll
-            for (int i = 0; i < NF; ++i)
-#pragma unroll
-                for (int f = 0; f < MF; ++f) acc[i][f] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
-            stream_products<T, NF, MF, D>(from, steps * wave / NW, steps * (wave + 1) / NW, pitch, lds + wave * kRing, acc);
+            for (int i = 0; i < NF; ++i) acc[i][0] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+            stream_products<T, NF, 1, D>(from, steps * wave / NW, steps * (wave + 1) / NW, pitch, lds + wave * kRing, acc);
             __syncthreads();  // the rings are done with
 #pragma unroll
-            for (int i = 0; i < NF; ++i)
-#pragma unroll
-                for (int f = 0; f < MF; ++f) part[((wave * NF + i) * MF + f) * kWave + lane] = acc[i][f];
+            for (int i = 0; i < NF; ++i) part[(wave * NF + i) * kWave + lane] = acc[i][0];
             __syncthreads();
-            for (int k = wave; k < NF * MF; k += NW) {  // a wave for each tile of the result
-                const int f = k % MF, n = n0 + k / MF * 16 + 4 * g;
-                floatx4 sum = part[k * kWave + lane];
+            if (wave < NF) {  // a wave for each tile of the result
+                const int n = n0 + wave * 16 + 4 * g;
+                floatx4 sum = part[wave * kWave + lane];
 #pragma unroll
-                for (int w = 1; w < NW; ++w) sum += part[(w * NF * MF + k) * kWave + lane];
-                if (__shfl(row_id, f * 16 + r) == ad && n < max_rank) {
+                for (int w = 1; w < NW; ++w) sum += part[(w * NF + wave) * kWave + lane];
+                if (__shfl(row_id, r) == ad && n < max_rank) {
                     float out[4];
 #pragma unroll
                     for (int u = 0; u < 4; ++u) out[u] = n + u < rank ? scale * sum[u] : 0.0f;
-                    io<T>::store4(reinterpret_cast<T *>(v + (row0 + f * 16 + r) * v_pitch) + n, out);
+                    io<T>::store4(reinterpret_cast<T *>(v + (row0 + r) * v_pitch) + n, out);
                 }
             }
             __syncthreads();

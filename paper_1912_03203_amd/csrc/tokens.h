@@ -37,7 +37,10 @@ int route_rows_per_group(int64_t tokens, int top_k) {
     return static_cast<int>(std::min<int64_t>(per, kRouteChunk / top_k));
 }
 
-bool route_is_one(int64_t tokens, int top_k) { return tokens <= 256 && tokens * top_k <= kRouteOne; }
+// One workgroup does it all up to 128 rows, two passes of its groups of lanes (64
+// rows of 64 experts, top 8: 7.5 us against 11.3 in three launches; 128: 11.2
+// against 11.4; 256: 18.6 against 11.5).
+bool route_is_one(int64_t tokens, int top_k) { return tokens <= 128 && tokens * top_k <= kRouteOne; }
 
 struct RouteLayout {
     int per = 0;
@@ -110,8 +113,8 @@ int64_t most_tiles(int64_t rows, int64_t groups, int bm, bool split) {
     return split ? rows / bm + std::min(rows, groups) : (rows + bm - 1) / bm;
 }
 
-// The forms of the products: few rows a group (16, 32 or 64 rows a workgroup,
-// weights straight to the matrix cores) or tiles through LDS.
+// The forms of the products: few rows a group (16 to 64 rows a workgroup, the
+// contraction split over its waves) or tiles of 64, 128 or 256 rows.
 struct RowsPlan {
     int bm = 0;      // rows of a tile
     int slices = 0;  // tiles along the outputs
@@ -119,23 +122,37 @@ struct RowsPlan {
     int64_t blocks = 0;
 };
 
+// The form by the mean number of rows a group and the tiles that groups of that
+// size make (weight rows = outputs, twice as many when gated); bf16, us:
+//   few rows / 64-row tiles   32 groups 2048 -> 1024, 16 rows each 25.7 / 26.8, 32:
+//     28.3 / 28.4, 64: 47.6 / 34.1; 8 groups 1024 -> 2048, 32 rows 10.4 / 9.1.  Few
+//     rows up to 16, and beyond where the tiles would leave most CUs idle (a decoding
+//     step through one projection).
+//   64 / 128  one group of 1024 rows 2048 -> 2048 (128 tiles of 128) 20.1 / 25.0, of
+//     2048 rows (256 tiles) 36.6 / 28.3; 12 groups of 125, 1024 -> 1024 (96) 12.7 / 15.9;
+//     32 of 96, 2048 -> 1024 (256) 50.5 / 38.0.  The larger tile from 192 on.
+//   128 / 256  one group of 2048 rows 2048 -> 4096 (128 tiles of 256) 46.2 / 48.7; 32
+//     groups of 256 rows 1024 -> 2048 (256 tiles) 59.9 / 48.2.  Likewise.  fp32 has no
+//     256-row tile: its products take 16 times as long, and fill the CUs with less.
 RowsPlan rows_plan(int64_t rows, int64_t groups, bool adapt, int c_out, bool gated, dynconv_dtype dt) {
-    const bool split = !adapt;  // into groups of sizes that only the device knows
     RowsPlan p;
-    const int64_t mean = (rows + groups - 1) / groups;
-    p.few = mean <= 64;
+    const int64_t mean = (rows + groups - 1) / groups, used = std::min(rows, groups);
+    const int64_t weights = static_cast<int64_t>(c_out) * (gated ? 2 : 1);
+    auto tiles = [&](int bm) { return used * ((mean + bm - 1) / bm) * ((weights + bm - 1) / bm); };
+    constexpr int64_t kFill = 192;  // tiles that keep the 256 CUs busy
+    p.few = mean <= 16 || (mean <= 64 && tiles(64) < kFill);
     if (p.few) {
         p.bm = static_cast<int>((mean + 15) / 16 * 16);
         const int outs = gated || adapt ? 16 : 32;
         p.slices = (c_out + outs - 1) / outs;
     } else {
-        const int64_t outs256 = static_cast<int64_t>(c_out) * (gated ? 2 : 1) / 256;
-        p.bm = dt != DYNCONV_F32 && mean >= 256 && rows / 256 * outs256 >= 192 ? 256
-               : rows / 128 * c_out * (gated ? 2 : 1) / 128 >= 256 ? 128 : 64;
+        p.bm = dt != DYNCONV_F32 && mean >= 256 && tiles(256) >= kFill ? 256 : tiles(128) >= kFill ? 128 : 64;
         const int outs = gated ? p.bm / 2 : p.bm;
         p.slices = (c_out + outs - 1) / outs;
     }
-    p.blocks = (most_tiles(rows, groups, p.bm, split) * p.slices + 7) / 8 * 8;  // whole turns of the 8 XCDs
+    // adapters: one group, of all rows; otherwise groups of sizes that only the
+    // device knows.  Whole turns of the 8 XCDs.
+    p.blocks = (most_tiles(rows, groups, p.bm, !adapt) * p.slices + 7) / 8 * 8;
     return p;
 }
 
@@ -254,28 +271,19 @@ size_t adapter_bytes(const dynconv_adapters *a, int64_t rows, dynconv_dtype dt) 
 template <typename T>
 void launch_adapters(const RowsArgs &args, const RowsPlan &p, const dynconv_linear *l, const dynconv_adapters *ad,
                      void *v, hipStream_t st, Marks &mk) {
-    // 32 rows a workgroup where that leaves one for every CU (an adapter's rows
-    // are then read half as often), else 16, with a workgroup for each distinct
-    // adapter that 16 rows can have
-    const bool wide = args.rows >= 32 * 128;
-    const int64_t tiles = (args.rows + (wide ? 31 : 15)) / (wide ? 32 : 16);
-    const unsigned turns = static_cast<unsigned>(tiles >= 256 || wide ? 1 : std::min<int64_t>({16, args.rows, ad->adapters}));
+    // 16 rows a workgroup, and one for each distinct adapter that 16 rows can have
+    // until they fill the CUs
+    const int64_t tiles = (args.rows + 15) / 16;
     dim3 grid = grid_xy(tiles);
-    grid.z = turns;
-    auto go = [&](auto kern, int waves) {
-        launch(mk, kern, grid, dim3(waves * kWave), 0, st, args.x, args.rows, args.pitch,
+    grid.z = static_cast<unsigned>(tiles >= 256 ? 1 : std::min<int64_t>({16, args.rows, ad->adapters}));
+    auto go = [&](auto kern) {
+        launch(mk, kern, grid, dim3(kDownWaves * kWave), 0, st, args.x, args.rows, args.pitch,
                static_cast<const char *>(ad->down), args.ids, ad->ranks, ad->scales, ad->adapters, args.id_bits,
                ad->max_rank, static_cast<char *>(v), args.v_pitch);
     };
-    if (wide) {
-        if (ad->max_rank <= 16) go(k_adapter_down<T, 8, 1, 2>, 8);
-        else if (ad->max_rank <= 32) go(k_adapter_down<T, 8, 2, 2>, 8);
-        else go(k_adapter_down<T, 4, 4, 2>, 4);
-    } else {
-        if (ad->max_rank <= 16) go(k_adapter_down<T, 8, 1, 1>, 8);
-        else if (ad->max_rank <= 32) go(k_adapter_down<T, 8, 2, 1>, 8);
-        else go(k_adapter_down<T, 8, 4, 1>, 8);
-    }
+    if (ad->max_rank <= 16) go(k_adapter_down<T, 1>);
+    else if (ad->max_rank <= 32) go(k_adapter_down<T, 2>);
+    else go(k_adapter_down<T, 4>);
     launch_rows<T, T, false, true>(args, p, st, mk);
 }
 
