@@ -255,7 +255,8 @@ __device__ __forceinline__ void choose_rows(const T *__restrict__ logits, int64_
     }
 }
 
-// Everything in one workgroup, for calls of up to kRouteOne assignments.
+// Everything in one workgroup, for calls of few rows: 5.4 us for 8 rows of 64
+// experts, top 8, the chain of a launch, one load, the rounds and four barriers.
 constexpr int kRouteOneThreads = 1024;
 constexpr int kRouteOne = 2048;
 
@@ -290,7 +291,14 @@ k_route_one(const T *__restrict__ logits, int tokens, int E, int top_k, int bits
     place_assignments<kRouteOneThreads>(ids, n, 0, E, bits, base, cnt, rows);
 }
 
-// Rows per workgroup of the two-launch form: at most kRouteChunk assignments.
+// Longer calls: choose and count, then add the counts up, then the lists; a
+// workgroup takes at most kRouteChunk assignments.  Choosing is bound by its vector
+// instructions: a round is some 60 of them for 4 rows a wave at 128 experts (the
+// largest of a lane's 8 keys, 4 steps over 16 lanes, the place of that key, 4 steps
+// for the lowest, its removal).  32768 rows of 128 fp32 logits, top 8: 14.0 us (16.8
+// MB: 3.3 us at the rate of a large copy), 7.4 us for the top 1; counts 4.0, lists
+// 6.5 us.  16 lanes a row do with a quarter of the steps of a whole wave; a lane's
+// experts are 16 apart, so that its loads cover whole lines.
 constexpr int kRouteChunk = 2048;
 
 template <typename T, int G, int V, int NT>

@@ -180,18 +180,22 @@ def test_grouped_activations(kind, rows):
     check_grouped((kind, rows, 1), rows, 2, 48, 40, TYPES[(kind + 1) % 3], kind=kind, bias=False)
 
 
-def test_grouped_large_tiles():
-    """A size that takes the largest tiles, odd edges on every side."""
-    gen = gen_for("large")
-    rows, groups, c_in, c_out = 5000, 3, 200, 4104
-    for dtype in TYPES[1:]:
-        starts = torch.tensor([0, 1111, 1111, 5000], dtype=torch.int32)
-        w = normal(gen, (groups, c_out, c_in), dtype, c_in ** -0.5)
-        x = normal(gen, (rows, c_in), dtype)
-        y = dc.grouped_linear(dev(x), torch.empty((rows, c_out), dtype=dtype, device=DEV), dev(w), None, dev(starts))
-        for lo, hi, g in ((0, 1111, 0), (1111, 5000, 2)):
-            want, err = plain.linear(x[lo:hi], w[g], None)
-            within(y[lo:hi], want, plain.stored(want, err, dtype), "large")
+@pytest.mark.parametrize("rows,c_out,dtype", [(1700, 2000, t) for t in TYPES] + [(5000, 4104, t) for t in TYPES[1:]])
+def test_grouped_large_tiles(rows, c_out, dtype):
+    """Sizes that take 128- and 256-row tiles, odd edges on every side."""
+    gen = gen_for("large", rows)
+    groups, c_in = 3, 200
+    cut = rows // 3 - 17
+    starts = torch.tensor([0, cut, cut, rows], dtype=torch.int32)
+    w = normal(gen, (groups, c_out, c_in), dtype, c_in ** -0.5)
+    x = normal(gen, (rows, c_in), dtype)
+    b = torch.randn((groups, c_out), generator=gen)
+    src, dst = torch.randperm(rows, generator=gen), torch.randperm(rows, generator=gen)
+    y = dc.grouped_linear(dev(x), torch.empty((rows, c_out), dtype=dtype, device=DEV), dev(w), dev(b), dev(starts),
+                          src=dev(src.int()), dst=dev(dst.int()), act=dc.ACT_GELU).cpu()
+    for lo, hi, g in ((0, cut, 0), (cut, rows, 2)):
+        want, err = plain.linear(x[src[lo:hi]], w[g], b[g], plain.GELU)
+        within(y[dst[lo:hi]], want, plain.stored(want, err, dtype), "large")
 
 
 def test_grouped_skips_what_lists_do_not_name():
@@ -291,10 +295,10 @@ def test_experts(dtype, tokens, experts, top_k, c_in, hidden, c_out, gated, bias
     within(got, want, bound, "experts")
 
 
-@pytest.mark.parametrize("dtype", TYPES[1:])
-def test_experts_large_tiles(dtype):
-    """Enough rows and widths for the largest tiles, gated, with edges on every side."""
-    tokens, top_k = 3301, 2
+@pytest.mark.parametrize("tokens,dtype", [(900, t) for t in TYPES] + [(3301, t) for t in TYPES[1:]])
+def test_experts_large_tiles(tokens, dtype):
+    """Rows and widths for the 128- and 256-row tiles, gated, with edges on every side."""
+    top_k = 2
     x, weights, logits, mask = expert_case("large", tokens, 2, top_k, 72, 1096, 72, dtype, True, True, dc.ACT_SILU, 0.05)
     r = dc.route(dev(logits), top_k, mask=dev(mask))
     some = torch.cat([torch.arange(0, tokens, 97), torch.arange(tokens - 9, tokens)])
@@ -366,7 +370,7 @@ def test_adapters_in_any_order(order, rows):
 
 
 @pytest.mark.parametrize("rank,c_out,dtype", [(16, 72, torch.float16), (24, 4104, torch.bfloat16), (128, 136, torch.bfloat16),
-                                              (64, 72, torch.float32)])
+                                              (64, 72, torch.float32), (40, 1000, torch.bfloat16), (8, 1000, torch.float32)])
 def test_adapters_large_tiles(rank, c_out, dtype):
     gen = gen_for("adapters large", rank)
     rows, c_in, n = 4200, 136, 5
