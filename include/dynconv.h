@@ -571,7 +571,8 @@ dynconv_status dynconv_grouped_linear(const void *x, int64_t x_rows, void *y, in
  *   h = act(W_gate x + b_gate) * (W_expand x + b_expand)
  *   F_e(x) = W_project h + b_project
  *   w_expand, w_gate [experts][c_hidden][c_in]; w_project [experts][c_out][c_hidden]
- * h is rounded to the storage type, F_e(x) stays in fp32 until it is summed.
+ * h is rounded to the storage type (calls of few tokens keep twice its bits),
+ * F_e(x) stays in fp32 until it is summed.
  */
 typedef struct {
     int32_t c_in, c_hidden, c_out, experts;

@@ -115,8 +115,14 @@ def grouped(x, y, w, b, starts, src=None, src_div=1, dst=None, kind=NONE):
     return out, bound
 
 
-def experts(x, weights, expert, weight, residual=False):
-    """weights: dict w_expand, w_gate, w_project, b_* (None: absent), act."""
+def halved(y, err, dtype):
+    """The same for a value stored as two of dtype, the second what the first left."""
+    return err + UNIT[dtype] ** 2 * (y.abs() + err) + TINY[dtype]
+
+
+def experts(x, weights, expert, weight, residual=False, few=False):
+    """weights: dict w_expand, w_gate, w_project, b_* (None: absent), act.  few: a call
+    of so few tokens that the hidden rows keep two values of a 16-bit type."""
     tokens = x.shape[0]
     c_out = weights["w_project"].shape[1]
     y = torch.zeros((tokens, c_out), dtype=torch.float64)
@@ -137,7 +143,8 @@ def experts(x, weights, expert, weight, residual=False):
                 h, eh = v * g, v.abs() * eg + g.abs() * ev + eg * ev + MORE * EPS32 * (v * g).abs()
             else:
                 h, eh = linear(row, of("w_expand", e), of("b_expand", e), weights["act"])
-            o, eo = linear((h, stored(h, eh, x.dtype)), of("w_project", e), of("b_project", e))
+            keep = halved if few and x.dtype != torch.float32 else stored
+            o, eo = linear((h, keep(h, eh, x.dtype)), of("w_project", e), of("b_project", e))
             k = float(weight[t, j])
             y[t] += k * o[0]
             err[t] += abs(k) * eo[0]

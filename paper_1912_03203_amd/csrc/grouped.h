@@ -68,6 +68,7 @@ struct RowsArgs {
     char *y;               // rows that come out, c_out entries each
     int64_t y_rows;
     const int32_t *dst;    // or NULL: list position p writes row p
+    bool halves;           // few rows, 16-bit types: a row's entries, then what their rounding left
     // low-rank adapters: y += up[ids[row]] * v[row]
     const char *v;         // [rows][v_pitch bytes]
     int v_pitch;
@@ -188,6 +189,13 @@ __device__ __forceinline__ int64_t target_row(const RowsArgs &a, int64_t p) {
 template <typename OT>
 __device__ __forceinline__ void store_out(OT *p, const float v[4]) {
     io<OT>::store4(p, v);
+}
+
+// What is left of v when it is stored as OT; nothing beside NaN and infinities.
+template <typename OT>
+__device__ __forceinline__ float rest_of(float v) {
+    const float high = static_cast<float>(static_cast<OT>(v));
+    return fabsf(high) < __builtin_huge_valf() ? v - high : 0.0f;
 }
 
 // act(sum + bias) of 4 consecutive outputs, gated: act(gate) * value.
@@ -444,6 +452,16 @@ k_rows_few(RowsArgs a, int slices) {
         }
         float out[4];
         finish4<GATED>(a, t.group, nn, sum, sum2, out);
+        if constexpr (sizeof(OT) == 2 && !ADAPT) {
+            if (a.halves) {
+                OT *row = reinterpret_cast<OT *>(a.y) + to * 2 * a.c_out + nn;
+                store_out<OT>(row, out);
+#pragma unroll
+                for (int u = 0; u < 4; ++u) out[u] = rest_of<OT>(out[u]);
+                store_out<OT>(row + a.c_out, out);
+                continue;
+            }
+        }
         store_out<OT>(reinterpret_cast<OT *>(a.y) + to * a.c_out + nn, out);
     }
 }
@@ -775,7 +793,12 @@ k_combine(const float *__restrict__ o, const int32_t *__restrict__ expert, const
 // the same expert, so that nothing is lost by reading the weights for each.  A
 // workgroup takes one token and 16 outputs; a wave takes every NW-th slot and
 // streams its expert's rows, or with fewer slots than waves several waves a part of
-// the contraction each.  Slots and parts are added in their order, in fp32.  One
+// the contraction each.  Slots and parts are added in their order, in fp32.
+//
+// Of the 16 rows of a matrix instruction one is needed.  In 16-bit types h comes as
+// two halves (its rounding, and what that left) on rows 0 and 8, so h keeps twice
+// the storage type's bits for nothing: the result's own rounding is what remains,
+// where a rounded h adds an error as large (few outputs: 1.5 times the error).  One
 // token, 8 slots, 1024 -> 2048 bf16: 33.5 MB in 11.5 us against 13.5 for the grouped
 // product and the sum; two tokens with 8 of 64 experts, whole layer, 44.8 against 49.0.
 template <typename T, int NW>
@@ -791,6 +814,7 @@ k_project_tokens(const char *__restrict__ h, int64_t pitch, const int32_t *__res
     const int n0 = static_cast<int>(blockIdx.x % static_cast<unsigned>(slices)) * 16;
     const int steps = static_cast<int>((pitch + kStreamStep - 1) / kStreamStep);
     const int parts = top_k < NW ? NW / top_k : 1, mine = wave % parts;
+    constexpr bool kHalves = sizeof(T) == 2;
     for (int s = wave / parts; s < top_k; s += NW) {
         const int e = __builtin_amdgcn_readfirstlane(expert[t * top_k + s]);
         if (e < 0 || e >= experts) continue;
@@ -799,11 +823,19 @@ k_project_tokens(const char *__restrict__ h, int64_t pitch, const int32_t *__res
         for (int i = 0; i < 2; ++i) {
             const int n = n0 + i * 8 + stream_row();
             rows[i] = w + (static_cast<int64_t>(e) * c_out + (n < c_out ? n : c_out - 1)) * pitch;
-            rows[2 + i] = h + (t * top_k + s) * pitch;  // one row: every lane's
+            rows[2 + i] = h + ((t * top_k + s) * (kHalves ? 2 : 1) + (kHalves ? i : 0)) * pitch;  // rows 0-7, 8-15
         }
         floatx4 acc[1][1] = {{floatx4{0.0f, 0.0f, 0.0f, 0.0f}}};
         stream_products<T, 1, 1, D>(rows, steps * mine / parts, steps * (mine + 1) / parts, pitch, lds + wave * kRing, acc);
-        if (lane % 16 == 0) part[s * parts + mine][lane / 16] = acc[0][0];
+        floatx4 v = acc[0][0];
+        if constexpr (kHalves) {
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const float rest = __shfl_xor(v[u], 8);
+                v[u] = fabsf(v[u]) < __builtin_huge_valf() ? v[u] + rest : v[u];  // infinite weights: the first half says it
+            }
+        }
+        if (lane % 16 == 0) part[s * parts + mine][lane / 16] = v;
     }
     __syncthreads();
     const int n = n0 + 4 * static_cast<int>(threadIdx.x);

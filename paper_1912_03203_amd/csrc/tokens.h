@@ -213,14 +213,25 @@ dynconv_status check_experts(const dynconv_experts *e, dynconv_dtype dt, int64_t
     return DYNCONV_OK;
 }
 
+// Few tokens: one launch for the second product and the sum.  A token's experts
+// differ, so one token always gains; more do while their choices seldom meet.
+bool few_tokens(int64_t tokens, int top_k, int experts) {
+    return tokens == 1 || tokens * top_k * 2 <= experts;
+}
+
 struct ExpertsLayout {
     size_t out = 0, bytes = 0;  // hidden rows first, then the experts' outputs in fp32
 };
 
-ExpertsLayout experts_layout(const dynconv_experts *e, int64_t rows, dynconv_dtype dt) {
+ExpertsLayout experts_layout(const dynconv_experts *e, int64_t tokens, int top_k, dynconv_dtype dt) {
     ExpertsLayout L;
-    L.out = align_up(static_cast<size_t>(rows) * e->c_hidden * dtype_size(dt));
-    L.bytes = std::max(kAlign, L.out + align_up(static_cast<size_t>(rows) * e->c_out * sizeof(float)));
+    const size_t rows = static_cast<size_t>(tokens) * top_k;
+    if (few_tokens(tokens, top_k, e->experts)) {  // hidden rows alone: two halves in 16-bit types, fp32 as it is
+        L.bytes = std::max(kAlign, align_up(rows * e->c_hidden * sizeof(float)));
+        return L;
+    }
+    L.out = align_up(rows * e->c_hidden * dtype_size(dt));
+    L.bytes = std::max(kAlign, L.out + align_up(rows * e->c_out * sizeof(float)));
     return L;
 }
 
@@ -230,12 +241,6 @@ void launch_combine(const float *o, const dynconv_routes *r, const void *x, void
     const int64_t items = tokens * (C / 8);
     launch(mk, k_combine<T>, grid_xy((items + kBlock - 1) / kBlock), dim3(kBlock), 0, st, o, r->expert, r->weight,
            static_cast<const T *>(x), static_cast<T *>(y), tokens, C, top_k, experts);
-}
-
-// Few tokens: one launch for the second product and the sum.  A token's experts
-// differ, so one token always gains; more do while their choices seldom meet.
-bool few_tokens(int64_t tokens, int top_k, int experts) {
-    return tokens == 1 || tokens * top_k * 2 <= experts;
 }
 
 template <typename T>
@@ -368,7 +373,7 @@ dynconv_status dynconv_grouped_linear(const void *x, int64_t x_rows, void *y, in
 
 size_t dynconv_experts_workspace_bytes(int64_t tokens, const dynconv_experts *e, dynconv_dtype dt, int32_t top_k) {
     if (check_experts(e, dt, tokens, top_k, 0) != DYNCONV_OK) return 0;
-    return experts_layout(e, tokens * top_k, dt).bytes;
+    return experts_layout(e, tokens, top_k, dt).bytes;
 }
 
 dynconv_status dynconv_experts_forward(const void *x, void *y, int64_t tokens, dynconv_dtype dt,
@@ -387,7 +392,7 @@ dynconv_status dynconv_experts_forward(const void *x, void *y, int64_t tokens, d
     const size_t in_bytes = static_cast<size_t>(tokens) * e->c_in * s;
     const size_t out_bytes = static_cast<size_t>(tokens) * e->c_out * s;
     if (ranges_overlap(x, in_bytes, y, out_bytes) && !(x == y && e->c_in == e->c_out)) return DYNCONV_ERR_SHAPE;
-    const ExpertsLayout L = experts_layout(e, rows, dt);
+    const ExpertsLayout L = experts_layout(e, tokens, top_k, dt);
     if (!ws || ws_bytes < L.bytes) return DYNCONV_ERR_WORKSPACE;
     if (tokens == 0) return DYNCONV_OK;
     RowsArgs a{};
@@ -408,10 +413,14 @@ dynconv_status dynconv_experts_forward(const void *x, void *y, int64_t tokens, d
     a.y = static_cast<char *>(ws);
     a.y_rows = rows;
     const bool few = few_tokens(tokens, top_k, e->experts);
-    if (few) a.dst = routes->rows;  // hidden rows at their assignments, not in list order
+    if (few) {
+        a.dst = routes->rows;  // hidden rows at their assignments, not in list order
+        a.halves = dt != DYNCONV_F32;
+    }
     const bool gated = e->w_gate != nullptr;
-    const RowsPlan p1 = rows_plan(rows, e->experts, false, e->c_hidden, gated, dt);
+    const RowsPlan p1 = rows_plan(rows, e->experts, false, e->c_hidden, gated, dt);  // few tokens: few rows
     RowsArgs o = a;
+    o.halves = false;
     o.x = static_cast<const char *>(ws);
     o.x_rows = rows;
     o.pitch = static_cast<int64_t>(e->c_hidden) * static_cast<int64_t>(s);

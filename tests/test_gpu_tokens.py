@@ -295,6 +295,52 @@ def test_experts(dtype, tokens, experts, top_k, c_in, hidden, c_out, gated, bias
     within(got, want, bound, "experts")
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("tokens,experts,top_k,c_in,hidden,c_out,gated", [
+    (1, 8, 8, 72, 1096, 168, True), (1, 1, 1, 136, 40, 72, False), (2, 22, 4, 168, 1568, 168, True),
+    (3, 64, 10, 136, 264, 136, False), (8, 1024, 16, 64, 72, 64, True)])
+def test_experts_of_few_tokens_keep_the_hidden_rows(dtype, tokens, experts, top_k, c_in, hidden, c_out, gated):
+    """The bound without the hidden rows' rounding, which small results would go past:
+    it leaves the result's own."""
+    kind = dc.ACT_SILU if gated else dc.ACT_GELU
+    x, weights, logits, _ = expert_case(("few", tokens, experts), tokens, experts, top_k, c_in, hidden, c_out, dtype,
+                                        gated, True, kind)
+    r = dc.route(dev(logits), top_k)
+    want, bound = plain.experts(x, weights, r.expert.cpu(), r.weight.cpu(), few=True)
+    y = util.Guarded(tokens * c_out, dtype, math.nan)
+    call = dc.Experts(dev(x), y.t.view(tokens, c_out), device_weights(weights), r)
+    guard = util.Guarded(call.ws.numel(), torch.uint8)
+    call = dc.Experts(dev(x), y.t.view(tokens, c_out), device_weights(weights), r, ws=guard.t)
+    guard.t.fill_(0xFF)
+    got = call()
+    torch.cuda.synchronize()
+    assert y.intact() and guard.intact()
+    within(got, want, bound, "few tokens")
+
+
+def test_experts_of_few_tokens_beside_infinities():
+    """An infinite weight meets the second half of a hidden entry, which may be zero or of
+    the other sign: the result is still the formula's infinity; a hidden entry past fp16's
+    largest value is infinite alone."""
+    for dtype in TYPES[1:]:
+        x, weights, logits, _ = expert_case("inf", 1, 4, 1, 64, 64, 64, dtype, False, False, dc.ACT_RELU)
+        r = dc.route(dev(logits), 1)
+        e = int(r.expert[0, 0])
+        h = torch.relu(weights["w_expand"][e].double() @ x[0].double())
+        k = int(h.argmax())
+        weights["w_project"][e, 5, k] = math.inf
+        weights["w_project"][e, 6, k] = -math.inf
+        y = torch.zeros((1, 64), dtype=dtype, device=DEV)
+        got = dc.experts_forward(dev(x), y, device_weights(weights), r).cpu()[0]
+        assert got[5] == math.inf and got[6] == -math.inf and int(torch.isfinite(got).sum()) == 62
+        weights["w_project"][e, 5:7, k] = 1.0
+        weights["b_expand"] = torch.zeros((4, 64))
+        weights["b_expand"][e, k] = math.inf
+        weights["w_project"][e, :, k] = 0.5
+        got = dc.experts_forward(dev(x), y, device_weights(weights), r).cpu()[0]
+        assert bool((got == math.inf).all())
+
+
 @pytest.mark.parametrize("tokens,dtype", [(900, t) for t in TYPES] + [(3301, t) for t in TYPES[1:]])
 def test_experts_large_tiles(tokens, dtype):
     """Rows and widths for the 128- and 256-row tiles, gated, with edges on every side."""
