@@ -468,8 +468,8 @@ k_rows_few(RowsArgs a, int slices) {
 
 // ------------------------------------------------------------- many rows
 // Tiles of BM rows x BN outputs through LDS, 64 bytes of the contraction a
-// step, five steps of LDS: the loads run four steps ahead of the products.  A row's 4 chunks are stored at chunk ^ (row / 2 % 4),
-// so 8 neighbouring rows at one chunk cover all banks; the loads go straight to
+// step, five steps of LDS: the loads run four steps ahead of the products.  A
+// row's 4 chunks are stored at chunk ^ (row / 2 % 4), so 8 neighbouring rows at one chunk cover all banks; the loads go straight to
 // LDS, which fixes a lane's place there, so the swizzle is applied to the
 // address that each lane loads.  Gated: the outputs of a tile are 16 of the
 // value's and 16 of the gate's in turn, so a wave holds both.
@@ -797,9 +797,9 @@ k_combine(const float *__restrict__ o, const int32_t *__restrict__ expert, const
 //
 // Of the 16 rows of a matrix instruction one is needed.  In 16-bit types h comes as
 // two halves (its rounding, and what that left) on rows 0 and 8, so h keeps twice
-// the storage type's bits for nothing: the result's own rounding is what remains,
+// the storage type's bits for some 0.5 us: the result's own rounding is what remains,
 // where a rounded h adds an error as large (few outputs: 1.5 times the error).  One
-// token, 8 slots, 1024 -> 2048 bf16: 33.5 MB in 11.5 us against 13.5 for the grouped
+// token, 8 slots, 1024 -> 2048 bf16: 33.5 MB in 12.3 us against 13.5 for the grouped
 // product and the sum; two tokens with 8 of 64 experts, whole layer, 44.8 against 49.0.
 template <typename T, int NW>
 __global__ void __launch_bounds__(NW * kWave)
