@@ -628,7 +628,8 @@ size_t dynconv_adapter_workspace_bytes(int64_t rows, const dynconv_linear *l, co
  *   y[r] = act(W x[r] + b + scales[i] * up_i (down_i x[r]))
  * and y[r] = act(W x[r] + b) where ids[r] is outside 0 .. adapters - 1.  The
  * rows may come in any order; those of one request side by side run fastest.
- * scales[i] * down_i x[r] is rounded to the storage type.
+ * scales[i] * down_i x[r] is kept in twice the bits of a 16-bit storage type (where
+ * it passes the type's largest value it is infinite).
  *   x (device) [rows][c_in], y (device) [rows][c_out], not overlapping
  *   ids (device) int32 [rows]
  */

@@ -156,19 +156,23 @@ def experts(x, weights, expert, weight, residual=False, few=False):
     return y, stored(y, err, x.dtype)
 
 
-def adapted(x, w, b, down, up, ids, scales=None, ranks=None, kind=NONE):
+def adapted(x, w, b, down, up, ids, scales=None, ranks=None, kind=NONE, halves=False):
+    """halves: the first half of an adapter keeps two values of a 16-bit type, so that
+    twice as many terms are added to the projection's sum."""
     rows, n = x.shape[0], down.shape[0]
     y, bound = torch.zeros((rows, w.shape[0]), dtype=torch.float64), torch.zeros((rows, w.shape[0]), dtype=torch.float64)
-    for r in range(rows):
-        s, e = linear(x[r][None], w, b)
-        i = int(ids[r])
+    keep = halved if halves and x.dtype != torch.float32 else stored
+    for i in sorted(set(ids.tolist())):
+        at = torch.nonzero(ids == i).flatten()
+        s, e = linear(x[at], w, b)
         if 0 <= i < n:
             rank = down.shape[1] if ranks is None else max(0, min(int(ranks[i]), down.shape[1]))
             k = 1.0 if scales is None else float(scales[i])
-            v, ev = linear(x[r][None], down[i, :rank], None)
+            v, ev = linear(x[at], down[i, :rank], None)
             v, ev = k * v, abs(k) * ev
-            a, ea = linear((v, stored(v, ev, x.dtype)), up[i, :, :rank], None)
-            s, e = s + a, e + ea + MORE * EPS32 * (s.abs() + a.abs())
+            a, ea = linear((v, keep(v, ev, x.dtype)), up[i, :, :rank], None)
+            more = MORE + (2 * rank if halves else 0)
+            s, e = s + a, e + ea + more * EPS32 * (s.abs() + a.abs())
         s, e = act(s, kind), LIPSCHITZ[kind] * e
-        y[r], bound[r] = s[0], stored(s, e, x.dtype)[0]
+        y[at], bound[at] = s, stored(s, e, x.dtype)
     return y, bound

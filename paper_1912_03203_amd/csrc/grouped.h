@@ -70,7 +70,7 @@ struct RowsArgs {
     const int32_t *dst;    // or NULL: list position p writes row p
     bool halves;           // few rows, 16-bit types: a row's entries, then what their rounding left
     // low-rank adapters: y += up[ids[row]] * v[row]
-    const char *v;         // [rows][v_pitch bytes]
+    const char *v;         // [rows][v_pitch bytes], see add_adapters
     int v_pitch;
     const char *up;        // [adapters][c_out][max_rank]
     const int32_t *ids, *ranks;
@@ -236,6 +236,33 @@ __device__ __forceinline__ uint64_t drop_lanes(uint64_t set, int n) {
     return set;
 }
 
+// The second product takes v = scale * down x in the storage type, but a rounded v
+// adds a tenth to the result's error (bf16), so 16-bit types keep v as two halves: its
+// rounding, and what that left.  They lie chunk by chunk in turn, so a row of v has
+// 4 * max_rank bytes in every type, and a step of 64 bytes of it covers 16 ranks: four
+// chunks of fp32, or two of the first halves and two of the second, which meet the
+// same two chunks of up.
+constexpr int kStepRanks = 16;
+
+// The first rank of chunk c of a step's four, and whether it meets a second half.
+template <typename T> __device__ __forceinline__ int chunk_rank(int c) { return sizeof(T) == 2 ? c / 2 * 8 : c * 4; }
+template <typename T> __device__ __forceinline__ bool chunk_rest(int c) { return sizeof(T) == 2 && c % 2 != 0; }
+
+// A chunk of up as a second half meets it: without infinities and NaN, which the
+// first half has brought into the sum already.
+template <typename T>
+__device__ __forceinline__ u32x4 for_rest(u32x4 u, bool rest) {
+    if constexpr (sizeof(T) == 2) {
+        typedef uint16_t u16x8 __attribute__((ext_vector_type(8)));
+        constexpr uint16_t kInf = std::is_same<T, half_t>::value ? 0x7c00 : 0x7f80;
+        u16x8 v = __builtin_bit_cast(u16x8, u);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = rest && (v[e] & kInf) == kInf ? 0 : v[e];
+        return __builtin_bit_cast(u32x4, v);
+    }
+    return u;
+}
+
 // acc += up[id] * v over the distinct adapters of MF * 16 rows from row0 (row
 // l's adapter, or -1, in lane l) and the 16 outputs from n0.  Each adapter is one
 // more run of the contraction, with the rows of the others at zero; of the
@@ -244,7 +271,7 @@ __device__ __forceinline__ uint64_t drop_lanes(uint64_t set, int n) {
 template <typename T, int MF>
 __device__ __forceinline__ void add_adapters(const RowsArgs &a, int row_id, int64_t row0, int n0, int first, int of,
                                              floatx4 (&acc)[1][MF]) {
-    constexpr int kPer = 16 / static_cast<int>(sizeof(T)), kOnce = 4;
+    constexpr int kOnce = 4;
     const int lane = threadIdx.x % kWave, g = lane / 16, r = lane % 16;
     uint64_t left = drop_lanes(distinct_lanes(row_id, a.id_bits), first);
     int id[MF];
@@ -260,8 +287,8 @@ __device__ __forceinline__ void add_adapters(const RowsArgs &a, int row_id, int6
             most = rank[b] > most ? rank[b] : most;
             left = drop_lanes(left, of);
         }
-        for (int k0 = 0; k0 < most; k0 += 4 * kPer) {
-            const int k = k0 + g * kPer;
+        for (int k0 = 0; k0 < most; k0 += kStepRanks) {
+            const int k = k0 + chunk_rank<T>(g);
             const u32x4 none = {0, 0, 0, 0};
             u32x4 rv[MF], uv[kOnce];
 #pragma unroll
@@ -273,14 +300,15 @@ __device__ __forceinline__ void add_adapters(const RowsArgs &a, int row_id, int6
 #pragma unroll
             for (int f = 0; f < MF; ++f)
                 rv[f] = k < most && id[f] >= 0
-                            ? *reinterpret_cast<const u32x4 *>(a.v + (row0 + f * 16 + r) * a.v_pitch +
-                                                               k * static_cast<int>(sizeof(T)))
+                            ? *reinterpret_cast<const u32x4 *>(a.v + (row0 + f * 16 + r) * a.v_pitch + k0 * 4 + g * 16)
                             : none;
 #pragma unroll
-            for (int b = 0; b < kOnce; ++b)
+            for (int b = 0; b < kOnce; ++b) {
+                const u32x4 u = for_rest<T>(uv[b], chunk_rest<T>(g));
 #pragma unroll
                 for (int f = 0; f < MF; ++f)
-                    acc[0][f] = chunk_mma<T>(uv[b], id[f] == ad[b] && k < rank[b] ? rv[f] : none, acc[0][f]);
+                    acc[0][f] = chunk_mma<T>(u, id[f] == ad[b] && k < rank[b] ? rv[f] : none, acc[0][f]);
+            }
         }
     }
 }
@@ -544,7 +572,6 @@ k_rows_tile(RowsArgs a, int slices) {
     const char *zero = reinterpret_cast<const char *>(kZeroChunk);
     // The adapters: each distinct one of the tile's rows is more steps of the
     // contraction, v against up, with the other adapters' rows at zero.
-    constexpr int kPer = 16 / static_cast<int>(sizeof(T));
     int open[BM / kWave], ad = -1, rank = 0, k0 = 0;
     auto next_adapter = [&]() {
         ad = -1;
@@ -571,7 +598,7 @@ k_rows_tile(RowsArgs a, int slices) {
     if constexpr (ADAPT) {
         open_adapters();
         while (next_adapter())
-            if (rank > 0) steps += (rank + 4 * kPer - 1) / (4 * kPer);
+            if (rank > 0) steps += (rank + kStepRanks - 1) / kStepRanks;
         open_adapters();
         rank = 0;
     }
@@ -589,13 +616,13 @@ k_rows_tile(RowsArgs a, int slices) {
             if (step >= own_steps && step < steps) {
                 while (k0 >= rank)
                     if (!next_adapter()) break;
-                const int k = k0 + lchunk * kPer;
+                const int k = k0 + chunk_rank<T>(lchunk);
                 const T *up = reinterpret_cast<const T *>(a.up) + static_cast<int64_t>(ad) * a.c_out * a.max_rank + k;
 #pragma unroll
                 for (int i = 0; i < C::kLoadsX; ++i) {
                     const int64_t p = t.row0 + (wave * C::kLoadsX + i) * 16 + lrow;
                     const bool in = k < rank && adapter_of(a, p, p < t.end) == ad;
-                    from[i] = in ? a.v + p * a.v_pitch + k * static_cast<int>(sizeof(T)) : zero;
+                    from[i] = in ? a.v + p * a.v_pitch + k0 * 4 + lchunk * 16 : zero;
                 }
 #pragma unroll
                 for (int i = 0; i < C::kLoadsW; ++i) {
@@ -604,7 +631,7 @@ k_rows_tile(RowsArgs a, int slices) {
                     from[C::kLoadsX + i] =
                         k < rank ? reinterpret_cast<const char *>(up + static_cast<int64_t>(n) * a.max_rank) : zero;
                 }
-                k0 += 4 * kPer;
+                k0 += kStepRanks;
             }
         }
     };
@@ -652,38 +679,48 @@ k_rows_tile(RowsArgs a, int slices) {
         const bool have = i * kWave + lane < MF * 16 && p < t.end;
         target[i] = have && source_row(a, p) >= 0 ? static_cast<int>(target_row(a, p)) : -1;
     }
+    const bool second = C::kTwo && wave >= C::kWaves / 2;
     if constexpr (C::kTwo) {
-        const bool second = wave >= C::kWaves / 2;
         loads_barrier<(C::kAhead - 1) * C::kLoads>();
         if (second) __builtin_amdgcn_s_barrier();
         sources(C::kAhead);
-        for (int s = 0; s < steps; ++s) {
-            // Reading, and the loads of step s + kAhead, into the slot of step
-            // s - 1, which both groups have read.  (Among the products the loads
-            // hold up: a wave that waits for its turn to load cannot multiply.)
-            read();
-            unrolled<C::kLoads>(load);
-            to = after(to);
-            __builtin_amdgcn_sched_barrier(0);
-            loads_barrier<(C::kAhead - 1) * C::kLoads>();  // step s + 1 has landed
-            __builtin_amdgcn_sched_barrier(0);
-            __builtin_amdgcn_s_setprio(1);
-            sources(s + 1 + C::kAhead);
-            unrolled<NF>(multiply);
-            __builtin_amdgcn_s_setprio(0);
-            __builtin_amdgcn_sched_barrier(0);
-            __builtin_amdgcn_s_barrier();
-            __builtin_amdgcn_sched_barrier(0);
-        }
-        if (!second) __builtin_amdgcn_s_barrier();
-    } else {
-        for (int s = 0; s < steps; ++s) {
-            loads_barrier<(C::kAhead - 1) * C::kLoads>();  // step s has landed, step s - 1 is read
-            load_all(s + C::kAhead);
-            read();
-            unrolled<NF>(multiply);
-        }
     }
+    auto run = [&](int s0, int s1, auto products) {
+        for (int s = s0; s < s1; ++s) {
+            if constexpr (C::kTwo) {
+                // Reading, and the loads of step s + kAhead, into the slot of step
+                // s - 1, which both groups have read.  (Among the products the loads
+                // hold up: a wave that waits for its turn to load cannot multiply.)
+                read();
+                unrolled<C::kLoads>(load);
+                to = after(to);
+                __builtin_amdgcn_sched_barrier(0);
+                loads_barrier<(C::kAhead - 1) * C::kLoads>();  // step s + 1 has landed
+                __builtin_amdgcn_sched_barrier(0);
+                __builtin_amdgcn_s_setprio(1);
+                sources(s + 1 + C::kAhead);
+                products();
+                __builtin_amdgcn_s_setprio(0);
+                __builtin_amdgcn_sched_barrier(0);
+                __builtin_amdgcn_s_barrier();
+                __builtin_amdgcn_sched_barrier(0);
+            } else {
+                loads_barrier<(C::kAhead - 1) * C::kLoads>();  // step s has landed, step s - 1 is read
+                load_all(s + C::kAhead);
+                read();
+                products();
+            }
+        }
+    };
+    run(0, own_steps, [&]() { unrolled<NF>(multiply); });
+    if constexpr (ADAPT)
+        run(own_steps, steps, [&]() {
+#pragma unroll
+            for (int i = 0; i < NF; ++i) wv[i] = for_rest<T>(wv[i], chunk_rest<T>(g));
+            unrolled<NF>(multiply);
+        });
+    if constexpr (C::kTwo)
+        if (!second) __builtin_amdgcn_s_barrier();
     loads_barrier<0>();  // LDS is free: each wave takes its share for its sums
 
     // The sums go through LDS in fp32 (16-byte chunk c of a row at c ^ row % 16),
@@ -862,9 +899,8 @@ k_project_tokens(const char *__restrict__ h, int64_t pitch, const int32_t *__res
 }
 
 // ------------------------------------------------ an adapter's first half
-// v[row] = scale * A_id x[row], rounded to the storage type (the matrix cores
-// take the second product's operand in it), for 16 rows a workgroup: one distinct
-// adapter of the rows at a time, every gridDim.z-th from blockIdx.z, NF tiles of 16
+// v[row] = scale * A_id x[row] as add_adapters takes it (16-bit types: in two
+// halves), for 16 rows a workgroup: one distinct adapter of the rows at a time, every gridDim.z-th from blockIdx.z, NF tiles of 16
 // of its rows.  The waves split the contraction, stream it, and add up through LDS
 // in wave order.  8192 rows of 4096 bf16, rank 32: 67 MB in 29 us, 2.3 TB/s (an
 // adapter's rows come from L2 for each 16 rows, four times as much); 32 rows a
@@ -925,7 +961,15 @@ k_adapter_down(const char *__restrict__ x, int64_t rows, int64_t pitch, const ch
                     float out[4];
 #pragma unroll
                     for (int u = 0; u < 4; ++u) out[u] = n + u < rank ? scale * sum[u] : 0.0f;
-                    io<T>::store4(reinterpret_cast<T *>(v + (row0 + r) * v_pitch) + n, out);
+                    if constexpr (sizeof(T) == 2) {  // chunk n / 8 of the first halves, and of the second
+                        T *to = reinterpret_cast<T *>(v + (row0 + r) * v_pitch) + n / 8 * 16 + n % 8;
+                        io<T>::store4(to, out);
+#pragma unroll
+                        for (int u = 0; u < 4; ++u) out[u] = rest_of<T>(out[u]);
+                        io<T>::store4(to + 8, out);
+                    } else {
+                        io<T>::store4(reinterpret_cast<T *>(v + (row0 + r) * v_pitch) + n, out);
+                    }
                 }
             }
             __syncthreads();

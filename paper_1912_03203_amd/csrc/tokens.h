@@ -269,8 +269,9 @@ dynconv_status check_adapters(const dynconv_linear *l, const dynconv_adapters *a
     return DYNCONV_OK;
 }
 
-size_t adapter_bytes(const dynconv_adapters *a, int64_t rows, dynconv_dtype dt) {
-    return std::max(kAlign, align_up(static_cast<size_t>(rows) * a->max_rank * dtype_size(dt)));
+// The first halves' results: fp32, or two halves of 16 bits.
+size_t adapter_bytes(const dynconv_adapters *a, int64_t rows) {
+    return std::max(kAlign, align_up(static_cast<size_t>(rows) * a->max_rank * sizeof(float)));
 }
 
 template <typename T>
@@ -460,7 +461,7 @@ dynconv_status dynconv_experts_forward(const void *x, void *y, int64_t tokens, d
 size_t dynconv_adapter_workspace_bytes(int64_t rows, const dynconv_linear *l, const dynconv_adapters *adapters,
                                        dynconv_dtype dt) {
     if (check_adapters(l, adapters, rows, dt) != DYNCONV_OK) return 0;
-    return adapter_bytes(adapters, rows, dt);
+    return adapter_bytes(adapters, rows);
 }
 
 dynconv_status dynconv_adapter_linear(const void *x, void *y, int64_t rows, dynconv_dtype dt, const dynconv_linear *l,
@@ -473,7 +474,7 @@ dynconv_status dynconv_adapter_linear(const void *x, void *y, int64_t rows, dync
     const size_t s = dtype_size(dt);
     if (ranges_overlap(x, static_cast<size_t>(rows) * l->c_in * s, y, static_cast<size_t>(rows) * l->c_out * s))
         return DYNCONV_ERR_SHAPE;
-    if (!ws || ws_bytes < adapter_bytes(adapters, rows, dt)) return DYNCONV_ERR_WORKSPACE;
+    if (!ws || ws_bytes < adapter_bytes(adapters, rows)) return DYNCONV_ERR_WORKSPACE;
     if (rows == 0) return DYNCONV_OK;
     RowsArgs a{};
     a.x = static_cast<const char *>(x);
@@ -489,7 +490,7 @@ dynconv_status dynconv_adapter_linear(const void *x, void *y, int64_t rows, dync
     a.y = static_cast<char *>(y);
     a.y_rows = rows;
     a.v = static_cast<const char *>(ws);
-    a.v_pitch = adapters->max_rank * static_cast<int>(s);
+    a.v_pitch = adapters->max_rank * static_cast<int>(sizeof(float));
     a.up = static_cast<const char *>(adapters->up);
     a.ids = ids;
     a.ranks = adapters->ranks;

@@ -1,0 +1,68 @@
+"""Low-rank adapters on the GPU: what the first half keeps, requests that do not
+reach one another, and every form of the product with ranks, scales and rows in
+any order.  Against the 64-bit form of oracle/tokens.py and its bounds."""
+import math
+
+import pytest
+import torch
+
+from oracle import tokens as plain
+from paper_1912_03203_amd import dynconv as dc
+from tests import util
+from tests.test_gpu_tokens import DEV, TYPES, dev, gen_for, normal, within
+
+pytestmark = pytest.mark.gpu
+
+#: rows, c_out: 16, 32, 48 and 64 rows a workgroup, then 64-, 128- and (16-bit) 256-row tiles
+FORMS = [(7, 72), (31, 40), (45, 104), (60, 72), (300, 72), (4200, 1000), (4200, 4104)]
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _lib():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    dc.load()
+
+
+def case(key, rows, c_out, dtype, adapters=5, max_rank=24, c_in=72, shuffled=True, ranks=True):
+    """Adapters of all ranks, rows of all requests mixed, some of them without one."""
+    gen = gen_for("adapters", key, rows, c_out)
+    s = {"x": normal(gen, (rows, c_in), dtype), "w": normal(gen, (c_out, c_in), dtype, c_in ** -0.5),
+         "b": 0.2 * torch.randn(c_out, generator=gen), "down": normal(gen, (adapters, max_rank, c_in), dtype, c_in ** -0.5),
+         "up": normal(gen, (adapters, c_out, max_rank), dtype, max_rank ** -0.5),
+         "ids": torch.randint(-1, adapters, (rows,), generator=gen, dtype=torch.int32),
+         "scales": torch.rand(adapters, generator=gen) + 0.5,
+         "ranks": torch.randint(1, max_rank + 1, (adapters,), generator=gen, dtype=torch.int32) if ranks else None}
+    if not shuffled:
+        s["ids"] = s["ids"].sort().values
+    return s
+
+
+def call(s, kind=dc.ACT_NONE):
+    rows, c_out = s["x"].shape[0], s["w"].shape[0]
+    y = util.Guarded(rows * c_out, s["x"].dtype, math.nan)
+    adapters = dc.Adapters(dev(s["down"]), dev(s["up"]), dev(s["scales"]), dev(s["ranks"]))
+    f = dc.AdapterLinear(dev(s["x"]), y.t.view(rows, c_out), dev(s["w"]), dev(s["b"]), adapters, dev(s["ids"]), act=kind)
+    ws = util.Guarded(f.ws.numel(), torch.uint8)
+    ws.t.fill_(0xFF)  # NaN everywhere: what is not written must not count
+    f = dc.AdapterLinear(dev(s["x"]), y.t.view(rows, c_out), dev(s["w"]), dev(s["b"]), adapters, dev(s["ids"]), act=kind,
+                         ws=ws.t)
+    got = f()
+    torch.cuda.synchronize()
+    assert y.intact() and ws.intact()
+    return got
+
+
+def expect(s, kind=dc.ACT_NONE, **kw):
+    return plain.adapted(s["x"], s["w"], s["b"], s["down"], s["up"], s["ids"], s["scales"], s["ranks"], kind, **kw)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,c_out", FORMS)
+def test_the_first_half_keeps_its_bits(dtype, rows, c_out):
+    """The bound without the first half's rounding to the storage type, which small
+    results would go past: it leaves the result's own."""
+    s = case("bits", rows, c_out, dtype, max_rank=40, ranks=False)
+    s["w"] = s["w"] * 0.125  # the adapters are what counts
+    want, bound = expect(s, halves=True)
+    within(call(s), want, bound, "first half")
