@@ -605,10 +605,9 @@ dynconv_status dynconv_experts_forward(const void *x, void *y, int64_t tokens, d
  * Low-rank adapters (device arrays), one per id:
  *   down [adapters][max_rank][c_in], up [adapters][c_out][max_rank] in the
  *   storage dtype, max_rank a multiple of 8 up to 256; ranks int32 [adapters]
- *   or NULL (all max_rank): rows of down from ranks[i] on are not read, columns
- *   of up from ranks[i] on do not count; scales fp32 [adapters] or NULL (1).
- *   up has to be finite throughout: rows without an adapter are multiplied with
- *   it as zeros, so that an infinity or NaN in it could reach rows beside its own
+ *   or NULL (all max_rank): rows of down and columns of up from ranks[i] on do
+ *   not count, whatever they hold; scales fp32 [adapters] or NULL (1).  An
+ *   infinity or NaN in an adapter stays in its own rows
  */
 typedef struct {
     int32_t adapters, max_rank;

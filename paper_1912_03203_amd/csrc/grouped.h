@@ -224,6 +224,48 @@ __device__ __forceinline__ int adapter_of(const RowsArgs &a, int64_t row, bool i
     return id >= 0 && id < a.adapters ? id : -1;
 }
 
+// The adapter of a row and its rank in one number, or -1 where nothing is added.
+constexpr int kAdapterBits = 20;
+constexpr int kMaxAdapters = 1 << kAdapterBits;
+__device__ __forceinline__ int adapter_key(const RowsArgs &a, int64_t row, bool in) {
+    const int id = adapter_of(a, row, in), rank = id < 0 ? 0 : adapter_rank(a, id);
+    return rank > 0 ? rank << kAdapterBits | id : -1;
+}
+
+// The distinct adapters of a tile of BM rows (row i * 64 + l's key in keys[i] of lane
+// l), in the order of their first rows; each wave walks by itself, over numbers that
+// all its lanes share.
+template <int BM>
+struct AdapterWalk {
+    uint64_t open[BM / kWave];  // rows of the adapters to come
+    uint64_t own;               // this adapter's rows of the 64 that `next` is asked for
+    int id, rank, k0;           // k0: its next rank
+    __device__ __forceinline__ void start(const int (&keys)[BM / kWave]) {
+#pragma unroll
+        for (int i = 0; i < BM / kWave; ++i) open[i] = __ballot(keys[i] >= 0);
+        own = 0;
+        id = rank = k0 = 0;
+    }
+    __device__ __forceinline__ bool next(const int (&keys)[BM / kWave], int block) {
+        int key = -1;
+#pragma unroll
+        for (int i = 0; i < BM / kWave; ++i)
+            if (open[i] && key < 0)
+                key = __builtin_amdgcn_readlane(keys[i], __ffsll(static_cast<unsigned long long>(open[i])) - 1);
+        if (key < 0) return false;
+#pragma unroll
+        for (int i = 0; i < BM / kWave; ++i) {
+            const uint64_t same = __ballot(keys[i] == key);
+            open[i] &= ~same;
+            own = i == block ? same : own;
+        }
+        id = key & (kMaxAdapters - 1);
+        rank = key >> kAdapterBits;
+        k0 = 0;
+        return true;
+    }
+};
+
 // The distinct adapters of up to 64 rows, row l's (or -1) in lane l: the lanes
 // that hold the first row of each.
 __device__ __forceinline__ uint64_t distinct_lanes(int id, int bits) {
@@ -248,24 +290,40 @@ constexpr int kStepRanks = 16;
 template <typename T> __device__ __forceinline__ int chunk_rank(int c) { return sizeof(T) == 2 ? c / 2 * 8 : c * 4; }
 template <typename T> __device__ __forceinline__ bool chunk_rest(int c) { return sizeof(T) == 2 && c % 2 != 0; }
 
-// A chunk of up as a second half meets it: without infinities and NaN, which the
-// first half has brought into the sum already.
+// A chunk of up without its infinities and NaN; odd gets a bit where there was one.
 template <typename T>
-__device__ __forceinline__ u32x4 for_rest(u32x4 u, bool rest) {
-    if constexpr (sizeof(T) == 2) {
-        typedef uint16_t u16x8 __attribute__((ext_vector_type(8)));
-        constexpr uint16_t kInf = std::is_same<T, half_t>::value ? 0x7c00 : 0x7f80;
-        u16x8 v = __builtin_bit_cast(u16x8, u);
+__device__ __forceinline__ u32x4 finite_part(u32x4 u, uint32_t &odd) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = rest && (v[e] & kInf) == kInf ? 0 : v[e];
-        return __builtin_bit_cast(u32x4, v);
+    for (int j = 0; j < 4; ++j) {
+        uint32_t m;  // all bits of such an entry
+        if constexpr (sizeof(T) == 4) {
+            m = static_cast<uint32_t>(static_cast<int32_t>((u[j] & 0x7fffffffu) + 0x00800000u) >> 31);
+        } else {
+            typedef int16_t i16x2 __attribute__((ext_vector_type(2)));
+            constexpr uint32_t kPast = std::is_same<T, half_t>::value ? 0x04000400u : 0x00800080u;
+            m = __builtin_bit_cast(uint32_t, __builtin_bit_cast(i16x2, (u[j] & 0x7fff7fffu) + kPast) >> 15);
+        }
+        u[j] &= ~m;
+        odd |= m;
+    }
+    return u;
+}
+
+// Its first `keep` entries, then zeros: the columns past a rank do not count.
+template <typename T>
+__device__ __forceinline__ u32x4 used_part(u32x4 u, int keep) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        if constexpr (sizeof(T) == 4) u[j] = keep > j ? u[j] : 0u;
+        else u[j] = keep > 2 * j + 1 ? u[j] : keep > 2 * j ? u[j] & 0xffffu : 0u;
     }
     return u;
 }
 
 // acc += up[id] * v over the distinct adapters of MF * 16 rows from row0 (row
 // l's adapter, or -1, in lane l) and the 16 outputs from n0.  Each adapter is one
-// more run of the contraction, with the rows of the others at zero; of the
+// more run of the contraction, whose sums only its own rows take (zeros for the
+// others' v would not do: an infinity or NaN in up makes NaN of them); of the
 // adapters, every `of`-th from `first` is taken (waves share the work), four at a
 // time, so that the loads of four are in flight.
 template <typename T, int MF>
@@ -304,11 +362,34 @@ __device__ __forceinline__ void add_adapters(const RowsArgs &a, int row_id, int6
                             : none;
 #pragma unroll
             for (int b = 0; b < kOnce; ++b) {
-                const u32x4 u = for_rest<T>(uv[b], chunk_rest<T>(g));
+                u32x4 u = used_part<T>(uv[b], rank[b] - k);
+                uint32_t odd = 0;
+                if (chunk_rest<T>(g)) u = finite_part<T>(u, odd);  // the first halves have brought the rest
 #pragma unroll
-                for (int f = 0; f < MF; ++f)
-                    acc[0][f] = chunk_mma<T>(u, id[f] == ad[b] && k < rank[b] ? rv[f] : none, acc[0][f]);
+                for (int f = 0; f < MF; ++f) {
+                    const floatx4 sum = chunk_mma<T>(u, k < rank[b] ? rv[f] : none, acc[0][f]);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) acc[0][f][e] = id[f] == ad[b] ? sum[e] : acc[0][f][e];
+                }
             }
+        }
+    }
+}
+
+// more += what the infinities and NaN in up give for one row and N outputs from n.
+template <typename T, int N>
+__device__ __forceinline__ void odd_products(const RowsArgs &a, int64_t row, int64_t end, int n, float (&more)[N]) {
+    const int key = adapter_key(a, row, row < end);
+    if (key < 0) return;
+    const T *up = reinterpret_cast<const T *>(a.up) +
+                  (static_cast<int64_t>(key & (kMaxAdapters - 1)) * a.c_out + n) * a.max_rank;
+    const T *v = reinterpret_cast<const T *>(a.v + row * a.v_pitch);
+    for (int k = 0; k < key >> kAdapterBits; ++k) {
+        const float by = static_cast<float>(v[sizeof(T) == 2 ? k / 8 * 16 + k % 8 : k]);
+#pragma unroll
+        for (int u = 0; u < N; ++u) {
+            const float w = static_cast<float>(up[u * a.max_rank + k]);
+            if (!(fabsf(w) < __builtin_huge_valf())) more[u] += w * by;
         }
     }
 }
@@ -571,36 +652,22 @@ k_rows_tile(RowsArgs a, int slices) {
     const uint32_t xl = lds0 + wave * C::kLoadsX * 1024, wl = lds0 + BM * 64 + wave * C::kLoadsW * 1024;
     const char *zero = reinterpret_cast<const char *>(kZeroChunk);
     // The adapters: each distinct one of the tile's rows is more steps of the
-    // contraction, v against up, with the other adapters' rows at zero.
-    int open[BM / kWave], ad = -1, rank = 0, k0 = 0;
-    auto next_adapter = [&]() {
-        ad = -1;
-#pragma unroll
-        for (int i = 0; i < BM / kWave; ++i) {
-            const uint64_t left = __ballot(open[i] >= 0);
-            if (left && ad < 0)
-                ad = __builtin_amdgcn_readlane(open[i], __ffsll(static_cast<unsigned long long>(left)) - 1);
-        }
-        if (ad < 0) return false;
-#pragma unroll
-        for (int i = 0; i < BM / kWave; ++i) open[i] = open[i] == ad ? -1 : open[i];
-        rank = adapter_rank(a, ad);
-        k0 = 0;
-        return true;
-    };
-    auto open_adapters = [&]() {
+    // contraction, v against up, with the other adapters' rows at zero.  The rows' ids
+    // and ranks are read once, here: a read among the steps would wait for the loads
+    // that run ahead as well (777 rows of 48 requests in any order: 82 against 95 us).
+    int keys[BM / kWave];
+    AdapterWalk<BM> ahead, now;  // at the step whose loads are next, at the one that is multiplied
+    const int my_rows = wave * C::kLoadsX / 4;  // the 64 rows that this wave's loads belong to
+    if constexpr (ADAPT) {
 #pragma unroll
         for (int i = 0; i < BM / kWave; ++i) {
             const int64_t p = t.row0 + i * kWave + lane;
-            open[i] = adapter_of(a, p, p < t.end);
+            keys[i] = adapter_key(a, p, p < t.end);
         }
-    };
-    if constexpr (ADAPT) {
-        open_adapters();
-        while (next_adapter())
-            if (rank > 0) steps += (rank + kStepRanks - 1) / kStepRanks;
-        open_adapters();
-        rank = 0;
+        ahead.start(keys);
+        while (ahead.next(keys, 0)) steps += (ahead.rank + kStepRanks - 1) / kStepRanks;
+        ahead.start(keys);
+        now.start(keys);
     }
     // Where the loads of step `step` come from; past the last step zeros.  The
     // steps are taken in order.
@@ -614,24 +681,25 @@ k_rows_tile(RowsArgs a, int slices) {
         left -= 64;
         if constexpr (ADAPT) {
             if (step >= own_steps && step < steps) {
-                while (k0 >= rank)
-                    if (!next_adapter()) break;
-                const int k = k0 + chunk_rank<T>(lchunk);
-                const T *up = reinterpret_cast<const T *>(a.up) + static_cast<int64_t>(ad) * a.c_out * a.max_rank + k;
+                if (ahead.k0 >= ahead.rank) ahead.next(keys, my_rows);
+                const int k = ahead.k0 + chunk_rank<T>(lchunk);
+                const T *up =
+                    reinterpret_cast<const T *>(a.up) + static_cast<int64_t>(ahead.id) * a.c_out * a.max_rank + k;
 #pragma unroll
                 for (int i = 0; i < C::kLoadsX; ++i) {
-                    const int64_t p = t.row0 + (wave * C::kLoadsX + i) * 16 + lrow;
-                    const bool in = k < rank && adapter_of(a, p, p < t.end) == ad;
-                    from[i] = in ? a.v + p * a.v_pitch + k0 * 4 + lchunk * 16 : zero;
+                    const int row = (wave * C::kLoadsX + i) * 16 + lrow;
+                    const bool in = k < ahead.rank && (ahead.own >> row % kWave & 1) != 0;
+                    from[i] = in ? a.v + (t.row0 + row) * a.v_pitch + ahead.k0 * 4 + lchunk * 16 : zero;
                 }
 #pragma unroll
                 for (int i = 0; i < C::kLoadsW; ++i) {
                     int n = n0 + (wave * C::kLoadsW + i) * 16 + lrow;
                     n = n < a.c_out ? n : a.c_out - 1;
-                    from[C::kLoadsX + i] =
-                        k < rank ? reinterpret_cast<const char *>(up + static_cast<int64_t>(n) * a.max_rank) : zero;
+                    from[C::kLoadsX + i] = k < ahead.rank
+                                               ? reinterpret_cast<const char *>(up + static_cast<int64_t>(n) * a.max_rank)
+                                               : zero;
                 }
-                k0 += kStepRanks;
+                ahead.k0 += kStepRanks;
             }
         }
     };
@@ -685,6 +753,21 @@ k_rows_tile(RowsArgs a, int slices) {
         if (second) __builtin_amdgcn_s_barrier();
         sources(C::kAhead);
     }
+    // A step of an adapter: its own rows' v, and zeros for the others.  Zeros would not
+    // keep an infinity or NaN in up from the others, so those entries are taken out
+    // here, and odd_products adds what they are to their own rows.
+    uint32_t odd = 0;
+    auto adapter_products = [&]() {
+        if (now.k0 >= now.rank) now.next(keys, 0);
+        const int left = now.rank - now.k0;
+        now.k0 += kStepRanks;
+        if (left < kStepRanks)
+#pragma unroll
+            for (int i = 0; i < NF; ++i) wv[i] = used_part<T>(wv[i], left - chunk_rank<T>(g));
+#pragma unroll
+        for (int i = 0; i < NF; ++i) wv[i] = finite_part<T>(wv[i], odd);
+        unrolled<NF>(multiply);
+    };
     auto run = [&](int s0, int s1, auto products) {
         for (int s = s0; s < s1; ++s) {
             if constexpr (C::kTwo) {
@@ -714,11 +797,7 @@ k_rows_tile(RowsArgs a, int slices) {
     };
     run(0, own_steps, [&]() { unrolled<NF>(multiply); });
     if constexpr (ADAPT)
-        run(own_steps, steps, [&]() {
-#pragma unroll
-            for (int i = 0; i < NF; ++i) wv[i] = for_rest<T>(wv[i], chunk_rest<T>(g));
-            unrolled<NF>(multiply);
-        });
+        run(own_steps, steps, adapter_products);
     if constexpr (C::kTwo)
         if (!second) __builtin_amdgcn_s_barrier();
     loads_barrier<0>();  // LDS is free: each wave takes its share for its sums
@@ -736,6 +815,7 @@ k_rows_tile(RowsArgs a, int slices) {
     const int col = lane % kLanes * kPerLane, n = n0 + (GATED ? wn / 2 : wn) + col;
     const int c0 = ((GATED ? col / 16 * 32 + col % 16 : col)) / 4;
     const bool in = n < a.c_out;
+    const bool any_odd = ADAPT && __ballot(odd != 0) != 0;
     float bias[kPerLane], bias2[kPerLane];
 #pragma unroll
     for (int u = 0; u < kPerLane; u += 4) {
@@ -759,7 +839,11 @@ k_rows_tile(RowsArgs a, int slices) {
         for (int row = lane / kLanes; row < kRows; row += kAtOnce) {
             const int to = __shfl(target[f0 * 16 / kWave], (f0 * 16 + row) % kWave);
             const char *from_row = mine + row * kRowBytes;
-            float out[kPerLane];
+            float out[kPerLane], more[kPerLane];
+#pragma unroll
+            for (int u = 0; u < kPerLane; ++u) more[u] = 0.0f;
+            if constexpr (ADAPT)
+                if (any_odd && in) odd_products<T, kPerLane>(a, t.row0 + wm + f0 * 16 + row, t.end, n, more);
 #pragma unroll
             for (int u = 0; u < kPerLane; u += 4) {
                 const int c = c0 + u / 4;
@@ -769,8 +853,9 @@ k_rows_tile(RowsArgs a, int slices) {
                     w = *reinterpret_cast<const floatx4 *>(from_row + ((c + 4) ^ (row & 15 & (kChunks - 1))) * 16);
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
-                    out[u + e] = GATED ? act_any(w[e] + bias2[u + e], a.act) * (v[e] + bias[u + e])
-                                       : act_any(v[e] + bias[u + e], a.act);
+                    out[u + e] = GATED   ? act_any(w[e] + bias2[u + e], a.act) * (v[e] + bias[u + e])
+                                 : ADAPT ? act_any(v[e] + more[u + e] + bias[u + e], a.act)
+                                         : act_any(v[e] + bias[u + e], a.act);
             }
             if (to >= 0 && in) {
                 OT *y = reinterpret_cast<OT *>(a.y) + static_cast<int64_t>(to) * a.c_out + n;

@@ -8,7 +8,6 @@ namespace {
 constexpr int64_t kMaxTokenRows = (int64_t{1} << 31) - 1;  // list entries are int32
 constexpr int kMaxWidth = 1 << 16;
 constexpr int kMaxRank = 256;
-constexpr int kMaxAdapters = 1 << 20;
 
 bool aligned4(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 
