@@ -522,7 +522,7 @@ size_t dynconv_route_workspace_bytes(int64_t tokens, int32_t experts, int32_t to
  *                          row that could be chosen; renormalised: over the
  *                          chosen ones (equal infinite maxima share alike)
  *   DYNCONV_ROUTE_SIGMOID: w = 1 / (1 + exp(-l)); renormalised: over the
- *                          chosen ones' sum (0 where that is 0)
+ *                          chosen ones' sum, also where each of them underflows
  * and weight = scale * w.  The choice and the lists are exact and
  * deterministic.
  *   logits (device) [tokens][experts], dtype dt, aligned to its type

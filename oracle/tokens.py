@@ -74,9 +74,12 @@ def route(logits, top_k, bias=None, mask=None, sigmoid=False, renormalize=False,
         if not chosen:
             continue
         if sigmoid:
-            s = [1 / (1 + math.exp(-v)) if v > -700 else 0.0 for v in (l[e] for e in chosen)]
+            # the sigmoids' logarithms, which do not underflow
+            logs = [v - math.log1p(math.exp(v)) if v < 0 else -math.log1p(math.exp(-v)) for v in (l[e] for e in chosen)]
+            top = max(logs) if renormalize else 0.0
+            s = [math.exp(v - top) for v in logs]
             total = sum(s) if renormalize else 1.0
-            w = [v / total if total else 0.0 for v in s]
+            w = [v / total for v in s]
         else:
             of = chosen if renormalize else live
             top = max(l[e] for e in of)

@@ -77,6 +77,12 @@ __device__ __forceinline__ uint32_t order_key(float v) {
 // exp(v - top) where equal infinities count as 1
 __device__ __forceinline__ float exp_below(float v, float top) { return v == top ? 1.0f : expf(v - top); }
 
+// 1 / (1 + exp(-v)) by the exponential that does not overflow
+__device__ __forceinline__ float sigmoid(float v) {
+    const float e = expf(-fabsf(v));
+    return (v < 0.0f ? e : 1.0f) / (1.0f + e);
+}
+
 // A row of logits on G lanes, V = ceil(E / G) experts a lane (expert v * G + lane).
 template <typename T, int G, int V>
 __device__ __forceinline__ void load_row(const T *__restrict__ row, bool on, int E, int lane, float (&l)[V]) {
@@ -130,9 +136,14 @@ __device__ __forceinline__ void choose_row(const float (&l)[V], const T *__restr
     weight = 0.0f;
     const float le = expert >= 0 ? static_cast<float>(row[expert]) : -__builtin_huge_valf();
     if (flags & kRouteSigmoid) {
-        const float s = expert >= 0 ? 1.0f / (1.0f + expf(-le)) : 0.0f;
-        const float sum = (flags & kRouteRenormalize) ? group_sumf<G>(s) : 1.0f;
-        if (s > 0.0f) weight = scale * (s / sum);
+        float s = sigmoid(le), sum = 1.0f;
+        if (flags & kRouteRenormalize) {
+            // all below 0: relative to the largest's, so that they do not all underflow
+            const float top = group_maxf<G>(le);
+            if (top < 0.0f) s = exp_below(le, top) * (1.0f + expf(top)) / (1.0f + expf(le));
+            sum = group_sumf<G>(expert >= 0 ? s : 0.0f);
+        }
+        if (expert >= 0) weight = scale * (s / sum);
     } else {
         const float top = whole ? all_top : group_maxf<G>(le);
         const float p = expert >= 0 ? exp_below(le, top) : 0.0f;
