@@ -33,7 +33,7 @@ def act(v, kind):
     if kind == SILU:
         return v * torch.sigmoid(v)
     if kind == GELU:
-        return 0.5 * v * (1 + torch.erf(v / math.sqrt(2)))
+        return 0.5 * v * torch.erfc(-v / math.sqrt(2))
     return v
 
 
