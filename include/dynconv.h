@@ -509,6 +509,7 @@ typedef struct {
 
 #define DYNCONV_ROUTE_SIGMOID 1     /* weights by sigmoid instead of softmax */
 #define DYNCONV_ROUTE_RENORMALIZE 2 /* weights of a row's chosen experts sum to `scale` */
+#define DYNCONV_ROUTE_SCORE_BIAS 8  /* bias is added to the scores, not to the logits */
 
 /* Workspace bytes of dynconv_route (0 for invalid sizes). */
 size_t dynconv_route_workspace_bytes(int64_t tokens, int32_t experts, int32_t top_k);
@@ -517,7 +518,13 @@ size_t dynconv_route_workspace_bytes(int64_t tokens, int32_t experts, int32_t to
  * Top-k router.  key[t][e] = logits[t][e] + bias[e], one fp32 addition; row t
  * takes the top_k experts of the largest keys, ties to the lowest e (-0 and +0
  * tie).  Experts whose key is NaN or -inf are never chosen, and a row whose
- * mask is 0 chooses none.  With l = the unbiased logits in fp32,
+ * mask is 0 chooses none.  With DYNCONV_ROUTE_SCORE_BIAS, the balancing bias of
+ * routers that add it to what their weights come from, key[t][e] = s + bias[e],
+ * s being the fp32 score 1 / (1 + exp(-l)) with DYNCONV_ROUTE_SIGMOID, else the
+ * softmax over the row's experts (a logit of NaN or -inf still takes no part);
+ * the two choices differ, as neither score is linear in the logits.  Without a
+ * bias the flag changes nothing.  A bias counts in the choice alone: with l =
+ * the unbiased logits in fp32,
  *   softmax:               w = exp(l) / sum of exp(l) over every expert of the
  *                          row that could be chosen; renormalised: over the
  *                          chosen ones (equal infinite maxima share alike)
@@ -528,7 +535,8 @@ size_t dynconv_route_workspace_bytes(int64_t tokens, int32_t experts, int32_t to
  *   logits (device) [tokens][experts], dtype dt, aligned to its type
  *   bias   (device) fp32 [experts], finite, or NULL
  *   mask   (device) uint8 [tokens] (nonzero = routed) or NULL: all rows
- *   flags  0 / DYNCONV_ROUTE_SIGMOID / DYNCONV_ROUTE_RENORMALIZE (others: ERR_ARG)
+ *   flags  any of DYNCONV_ROUTE_SIGMOID, DYNCONV_ROUTE_RENORMALIZE and
+ *          DYNCONV_ROUTE_SCORE_BIAS (others: ERR_ARG)
  *   1 <= experts <= 1024, 1 <= top_k <= min(16, experts)
  */
 dynconv_status dynconv_route(const void *logits, int64_t tokens, dynconv_dtype dt, int32_t experts, int32_t top_k,

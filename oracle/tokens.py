@@ -102,6 +102,27 @@ def route(logits, top_k, bias=None, mask=None, sigmoid=False, renormalize=False,
     return expert, weight, torch.tensor(rows, dtype=torch.int32), torch.tensor(starts, dtype=torch.int32)
 
 
+def route_of(logits, expert, mask=None, sigmoid=False, renormalize=False, scale=1.0):
+    """weight, rows and starts of a choice that is given (softmax over the experts whose
+    logits are neither NaN nor -inf)."""
+    l = logits.double()
+    there = expert >= 0
+    chosen = l.gather(1, expert.long().clamp(min=0)).masked_fill(~there, -math.inf)
+    of = chosen if renormalize else l.masked_fill(~(l > -math.inf), -math.inf)
+    score = torch.nn.functional.logsigmoid if sigmoid else (lambda v: v)
+    logs = score(chosen)
+    if sigmoid and not renormalize:
+        total = torch.zeros_like(logs[:, :1])
+    else:
+        total = torch.logsumexp(score(of), 1, keepdim=True)
+    weight = (scale * torch.exp(logs - total)).masked_fill(~there, 0.0)
+    flat = torch.where(there, expert.long(), logits.shape[1]).reshape(-1)
+    rows = torch.sort(flat, stable=True).indices
+    starts = (flat[None] < torch.arange(logits.shape[1] + 1)[:, None]).sum(1)
+    rows = torch.where(torch.arange(flat.numel()) < starts[-1], rows, -1)
+    return weight, rows.to(torch.int32), starts.to(torch.int32)
+
+
 def grouped(x, y, w, b, starts, src=None, src_div=1, dst=None, kind=NONE):
     """(y in 64 bits with the rows that no position names as they were, bound)."""
     out, bound = y.double().clone(), torch.zeros_like(y, dtype=torch.float64)

@@ -2,11 +2,12 @@
 // experts with the largest scores, their weights, and the lists that group the
 // assignments by expert, the many-way form of the mask unit and its index maps.
 //
-// Choice.  key = fl32(logit + bias); the k largest keys win, ties go to the
-// lowest expert.  An expert whose key is NaN or -inf, and every expert of a
-// masked row, is never chosen; a slot without an expert holds -1 and weight 0.
-// Keys are compared as integers that order like the floats, so the choice is
-// exact.  Weights are fp32: softmax with the maximum subtracted, or sigmoid.
+// Choice.  key = fl32(logit + bias), or the score (softmax or sigmoid, fp32) plus the
+// bias; the k largest keys win, ties go to the lowest expert.  An expert whose logit or
+// key is NaN or -inf, and every expert of a masked row, is never chosen; a slot without
+// an expert holds -1 and weight 0.  Keys are compared as integers that order like the
+// floats, so the choice is exact.  Weights are fp32: softmax with the maximum
+// subtracted, or sigmoid; a bias never counts in them.
 //
 // Lists.  Assignment a = row * k + slot.  A counting sort that keeps the order:
 // the choosing workgroups count their assignments per expert, and the list
@@ -23,7 +24,7 @@ constexpr int kMaxTopK = 16;
 constexpr int kRouteThreads = 512;
 constexpr int kRouteWaves = kRouteThreads / kWave;
 
-constexpr int kRouteSigmoid = 1, kRouteRenormalize = 2;
+constexpr int kRouteSigmoid = 1, kRouteRenormalize = 2, kRouteScoreBias = 8;
 
 // Reductions over G consecutive lanes (16 or 64); every lane gets the result.
 template <int CTRL>
@@ -102,21 +103,29 @@ __device__ __forceinline__ void choose_row(const float (&l)[V], const T *__restr
     uint32_t key[V];
     float all_top = -__builtin_huge_valf(), all_sum = 0.0f;
     const bool whole = !(flags & (kRouteSigmoid | kRouteRenormalize));  // softmax over every live expert
-    {
+    const bool by_score = bias && (flags & kRouteScoreBias);
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        const int e = v * G + lane;
+        key[v] = order_key(bias && !by_score && e < E ? l[v] + bias[e] : l[v]);
+    }
+    if (whole || (by_score && !(flags & kRouteSigmoid))) {
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+            if (key[v]) all_top = fmaxf(all_top, l[v]);
+        all_top = group_maxf<G>(all_top);
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+            if (key[v]) all_sum += exp_below(l[v], all_top);
+        all_sum = group_sumf<G>(all_sum);
+    }
+    if (by_score) {
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             const int e = v * G + lane;
-            key[v] = order_key(bias && e < E ? l[v] + bias[e] : l[v]);
-        }
-        if (whole) {
-#pragma unroll
-            for (int v = 0; v < V; ++v)
-                if (key[v]) all_top = fmaxf(all_top, l[v]);
-            all_top = group_maxf<G>(all_top);
-#pragma unroll
-            for (int v = 0; v < V; ++v)
-                if (key[v]) all_sum += exp_below(l[v], all_top);
-            all_sum = group_sumf<G>(all_sum);
+            if (!key[v]) continue;  // e < E
+            const float score = (flags & kRouteSigmoid) ? sigmoid(l[v]) : exp_below(l[v], all_top) / all_sum;
+            key[v] = order_key(score + bias[e]);
         }
     }
     expert = -1;

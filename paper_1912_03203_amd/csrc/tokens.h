@@ -309,7 +309,7 @@ dynconv_status dynconv_route(const void *logits, int64_t tokens, dynconv_dtype d
     if (!dtype_ok(dt)) return DYNCONV_ERR_DTYPE;
     if (dynconv_status st = check_route_sizes(tokens, experts, top_k)) return st;
     if (tokens > 0 && (!logits || !routes->expert || !routes->weight || !routes->rows)) return DYNCONV_ERR_NULL;
-    if (flags & ~(DYNCONV_ROUTE_SIGMOID | DYNCONV_ROUTE_RENORMALIZE)) return DYNCONV_ERR_ARG;
+    if (flags & ~(DYNCONV_ROUTE_SIGMOID | DYNCONV_ROUTE_RENORMALIZE | DYNCONV_ROUTE_SCORE_BIAS)) return DYNCONV_ERR_ARG;
     if (routes->capacity < tokens * top_k) return DYNCONV_ERR_CAPACITY;
     if ((reinterpret_cast<uintptr_t>(logits) & (dtype_size(dt) - 1)) != 0) return DYNCONV_ERR_ALIGN;
     for (const void *p : {static_cast<const void *>(bias), static_cast<const void *>(routes->expert),

@@ -559,7 +559,7 @@ class Network:
 
 # ---------------------------------------------------------- token operators
 ACT_SILU, ACT_GELU = 3, 4
-ROUTE_SIGMOID, ROUTE_RENORMALIZE = 1, 2
+ROUTE_SIGMOID, ROUTE_RENORMALIZE, ROUTE_SCORE_BIAS = 1, 2, 8
 EXPERTS_RESIDUAL = 1
 
 
@@ -690,7 +690,9 @@ class Routes:
 
 
 class Router(_Prepared):
-    """A prepared dynconv_route call: logits [T, experts] -> Routes."""
+    """A prepared dynconv_route call: logits [T, experts] -> Routes.  bias is added to
+    the logits, or with ROUTE_SCORE_BIAS to the scores (a balancing bias); it decides
+    who is chosen and does not count in the weights."""
 
     def __init__(self, logits, top_k, bias=None, mask=None, flags=0, scale=1.0, routes=None, ws=None):
         lib = load()

@@ -53,3 +53,65 @@ def test_sigmoid_shares_of_many_rows(dtype):
         want = plain.route(logits, top_k, None, None, True, True)
         assert torch.equal(r.expert.cpu(), want[0]) and torch.equal(r.rows.cpu(), want[2])
         within(r.weight, want[1], (2.0 ** -20 + 200 * plain.EPS32) * want[1] + 1e-37, "weight")
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_a_bias_on_the_scores_by_hand(dtype):
+    """Logits 4 and 2 with biases 0 and 0.15: sigmoids 0.982 and 0.881 + 0.15 = 1.031, so
+    the second expert, with its sigmoid as its weight; on the logits the first.  Softmax
+    of 1, 0, 0: 0.576, 0.212, 0.212; with biases 0, 0, 0.4 the third comes first."""
+    logits = torch.tensor([[4.0, 2.0]], dtype=dtype, device="cuda")
+    bias = torch.tensor([0.0, 0.15], device="cuda")
+    first = dc.route(logits, 1, bias=bias, flags=dc.ROUTE_SIGMOID)
+    second = dc.route(logits, 1, bias=bias, flags=dc.ROUTE_SIGMOID | dc.ROUTE_SCORE_BIAS)
+    assert first.expert.tolist() == [[0]] and second.expert.tolist() == [[1]]
+    assert abs(float(second.weight) - 1 / (1 + math.exp(-2.0))) < 1e-6
+    logits = torch.tensor([[1.0, 0.0, 0.0]], dtype=dtype, device="cuda")
+    bias = torch.tensor([0.0, 0.0, 0.4], device="cuda")
+    for flags, weights in ((0, [math.e / (math.e + 2), 1 / (math.e + 2)]),
+                           (dc.ROUTE_RENORMALIZE, [math.e / (math.e + 1), 1 / (math.e + 1)])):
+        r = dc.route(logits, 2, bias=bias, flags=flags | dc.ROUTE_SCORE_BIAS)
+        assert r.expert.tolist() == [[2, 0]]
+        assert abs(float(r.weight[0, 1]) - weights[0]) < 1e-6 and abs(float(r.weight[0, 0]) - weights[1]) < 1e-6
+
+
+def by_score(logits, top_k, bias, mask, sigmoid):
+    """Chosen experts by the scores in 64 bits, and the rows where no two of the scores
+    that decide come closer than an fp32 score's error: 6 roundings of a sigmoid and its
+    sum with the bias, or those of a sum of E exponentials (values of at most 2)."""
+    l = logits.double()
+    live = l > -math.inf
+    if sigmoid:
+        score = torch.sigmoid(l)
+    else:
+        score = torch.softmax(l.masked_fill(~live, -math.inf), 1)
+    score = (score + bias.double()).masked_fill(~live | (mask[:, None] == 0), -math.inf)
+    order = score.argsort(dim=1, descending=True, stable=True)
+    best = score.gather(1, order)[:, :top_k + 1]
+    near = (best[:, :-1] - best[:, 1:]).nan_to_num(nan=1.0).amin(1)
+    expert = torch.where(best[:, :top_k] == -math.inf, -1, order[:, :top_k]).to(torch.int32)
+    return expert, near > (logits.shape[1] + 16) * 2.0 ** -23
+
+
+@pytest.mark.parametrize("flags", range(4))
+@pytest.mark.parametrize("tokens,experts,top_k", [(1, 40, 6), (90, 17, 4), (700, 158, 6), (400, 64, 8), (300, 300, 3)])
+def test_a_bias_on_the_scores(tokens, experts, top_k, flags):
+    gen = gen_for("score bias", tokens, experts)
+    logits = normal(gen, (tokens, experts), TYPES[(tokens + flags) % 3], 2.0)
+    bias = 0.1 * torch.randn(experts, generator=gen)
+    mask = (torch.rand(tokens, generator=gen) > 0.1).to(torch.uint8)
+    if experts == 17:
+        logits[::3, 4], logits[::5, 2] = -math.inf, math.nan
+        logits[11] = -math.inf
+    want, apart = by_score(logits, top_k, bias, mask, bool(flags & 1))
+    assert int(apart.sum()) > 0.98 * tokens
+    r = dc.route(dev(logits), top_k, bias=dev(bias), mask=dev(mask), flags=flags | dc.ROUTE_SCORE_BIAS, scale=2.5)
+    expert = r.expert.cpu()
+    assert torch.equal(expert[apart], want[apart])
+    # the weights and the lists of what was chosen
+    weight, rows, starts = plain.route_of(logits, expert, mask, bool(flags & 1), bool(flags & 2), 2.5)
+    within(r.weight, weight, (2.0 ** -20 + (experts + 100) * plain.EPS32) * weight + 1e-37, "weight")
+    assert torch.equal(r.rows.cpu(), rows) and torch.equal(r.starts.cpu(), starts)
+    if flags & 2:  # without a bias the scores order the experts as the logits do
+        same = dc.route(dev(logits), top_k, mask=dev(mask), flags=flags | dc.ROUTE_SCORE_BIAS)
+        assert torch.equal(same.expert, dc.route(dev(logits), top_k, mask=dev(mask), flags=flags).expert)
