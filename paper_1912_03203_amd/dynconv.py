@@ -619,6 +619,19 @@ def _storage(x, name):
         raise DynconvError("%s: an fp32, fp16 or bf16 tensor is needed" % name)
 
 
+def _int32(v, name):
+    """v as it reaches the library: ctypes would cut a larger number to 32 bits."""
+    try:
+        n = int(v)
+    except (TypeError, ValueError, OverflowError):
+        n = None
+    if n is None or n != v:
+        raise DynconvError("%s: a whole number is needed, not %r" % (name, v))
+    if not -2**31 <= n < 2**31:
+        raise DynconvError("%s: %d does not fit in 32 bits" % (name, n))
+    return n
+
+
 class _Prepared:
     """A call marshalled once: calling it enqueues it on `stream` (default: the
     current stream of the tensors' device).  The object holds its tensors and its
@@ -699,6 +712,7 @@ class Router(_Prepared):
         _storage(logits, "logits")
         _need(logits, "logits", logits.dtype, (None, None), logits)
         tokens, experts = logits.shape
+        top_k, flags = _int32(top_k, "top_k"), _int32(flags, "flags")
         if bias is not None:
             _need(bias, "bias", torch.float32, (experts,), logits)
         if mask is not None:
@@ -711,7 +725,7 @@ class Router(_Prepared):
         self.struct = self.routes.struct()
         self._prepare(logits.device, lib.dynconv_route, "dynconv_route",
                       (_raw(logits), tokens, dtype_code(logits.dtype), experts, top_k, _raw(bias), _raw(mask),
-                       int(flags), float(scale), ctypes.byref(self.struct), self.ws.data_ptr(),
+                       flags, float(scale), ctypes.byref(self.struct), self.ws.data_ptr(),
                        self.ws.numel() * self.ws.element_size()))
 
     def _result(self):
@@ -759,10 +773,11 @@ class GroupedLinear(_Prepared):
             raise DynconvError("src and dst: %d and %d positions" % (src.numel(), dst.numel()))
         self.y = y
         self.keep = (x, y, w, b, starts, src, dst)
-        self.linear = LinearStruct(c_in, c_out, _raw(w), _raw(b), int(act))
+        self.linear = LinearStruct(c_in, c_out, _raw(w), _raw(b), _int32(act, "act"))
+        src_div = _int32(src_div, "src_div")
         self._prepare(x.device, lib.dynconv_grouped_linear, "dynconv_grouped_linear",
                       (_raw(x), x.shape[0], _raw(y), y.shape[0], dtype_code(x.dtype), ctypes.byref(self.linear), groups,
-                       _raw(starts), rows, _raw(src), int(src_div), _raw(dst)))
+                       _raw(starts), rows, _raw(src), src_div, _raw(dst)))
 
     def _result(self):
         return self.y
@@ -804,7 +819,7 @@ class ExpertWeights:
         n, h, c = self.w_expand.shape
         return ExpertsStruct(c, h, self.w_project.shape[1], n, _raw(self.w_expand), _raw(self.b_expand),
                              _raw(self.w_gate), _raw(self.b_gate), _raw(self.w_project), _raw(self.b_project),
-                             int(self.act))
+                             _int32(self.act, "act"))
 
 
 class Experts(_Prepared):
@@ -818,6 +833,7 @@ class Experts(_Prepared):
         _need(y, "y", x.dtype, (tokens, weights.w_project.shape[1]), x)
         top_k = routes.expert.shape[-1]
         routes.check(tokens, experts, top_k, x)
+        flags = _int32(flags, "flags")
         self.struct, self.rstruct = weights.struct(), routes.struct()
         code = dtype_code(x.dtype)
         nbytes = lib.dynconv_experts_workspace_bytes(tokens, ctypes.byref(self.struct), code, top_k)
@@ -826,7 +842,7 @@ class Experts(_Prepared):
         self.keep = (x, y, weights, routes)
         self._prepare(x.device, lib.dynconv_experts_forward, "dynconv_experts_forward",
                       (_raw(x), _raw(y), tokens, code, ctypes.byref(self.struct), top_k, ctypes.byref(self.rstruct),
-                       int(flags), self.ws.data_ptr(), self.ws.numel() * self.ws.element_size()))
+                       flags, self.ws.data_ptr(), self.ws.numel() * self.ws.element_size()))
 
     def _result(self):
         return self.y
@@ -877,7 +893,8 @@ class AdapterLinear(_Prepared):
         if b is not None:
             _need(b, "b", torch.float32, (c_out,), x)
         adapters.check(x, c_out)
-        self.linear, self.struct = LinearStruct(c_in, c_out, _raw(w), _raw(b), int(act)), adapters.struct()
+        self.linear = LinearStruct(c_in, c_out, _raw(w), _raw(b), _int32(act, "act"))
+        self.struct = adapters.struct()
         code = dtype_code(x.dtype)
         nbytes = lib.dynconv_adapter_workspace_bytes(rows, ctypes.byref(self.linear), ctypes.byref(self.struct), code)
         self.ws = _scratch(nbytes, ws, x.device, "dynconv_adapter_workspace_bytes")
