@@ -670,6 +670,11 @@ def _scratch(nbytes, ws, device, name):
     return ws
 
 
+def _tensors(d):
+    """The tensors of a dataclass as they are now: its fields may be given others."""
+    return tuple(t for t in vars(d).values() if isinstance(t, torch.Tensor))
+
+
 def _raw(t):
     return None if t is None or t.numel() == 0 else t.data_ptr()
 
@@ -721,7 +726,7 @@ class Router(_Prepared):
         self.ws = _scratch(nbytes, ws, logits.device, "dynconv_route_workspace_bytes")
         self.routes = Routes.alloc(tokens, experts, top_k, logits.device) if routes is None else routes
         self.routes.check(tokens, experts, top_k, logits)
-        self.keep = (logits, bias, mask)
+        self.keep = (logits, bias, mask) + _tensors(self.routes)
         self.struct = self.routes.struct()
         self._prepare(logits.device, lib.dynconv_route, "dynconv_route",
                       (_raw(logits), tokens, dtype_code(logits.dtype), experts, top_k, _raw(bias), _raw(mask),
@@ -839,7 +844,7 @@ class Experts(_Prepared):
         nbytes = lib.dynconv_experts_workspace_bytes(tokens, ctypes.byref(self.struct), code, top_k)
         self.ws = _scratch(nbytes, ws, x.device, "dynconv_experts_workspace_bytes")
         self.y = y
-        self.keep = (x, y, weights, routes)
+        self.keep = (x, y) + _tensors(weights) + _tensors(routes)
         self._prepare(x.device, lib.dynconv_experts_forward, "dynconv_experts_forward",
                       (_raw(x), _raw(y), tokens, code, ctypes.byref(self.struct), top_k, ctypes.byref(self.rstruct),
                        flags, self.ws.data_ptr(), self.ws.numel() * self.ws.element_size()))
@@ -899,7 +904,7 @@ class AdapterLinear(_Prepared):
         nbytes = lib.dynconv_adapter_workspace_bytes(rows, ctypes.byref(self.linear), ctypes.byref(self.struct), code)
         self.ws = _scratch(nbytes, ws, x.device, "dynconv_adapter_workspace_bytes")
         self.y = y
-        self.keep = (x, y, w, b, adapters, ids)
+        self.keep = (x, y, w, b, ids) + _tensors(adapters)
         self._prepare(x.device, lib.dynconv_adapter_linear, "dynconv_adapter_linear",
                       (_raw(x), _raw(y), rows, code, ctypes.byref(self.linear), ctypes.byref(self.struct), _raw(ids),
                        self.ws.data_ptr(), self.ws.numel() * self.ws.element_size()))
