@@ -743,15 +743,19 @@ def route(logits, top_k, bias=None, mask=None, flags=0, scale=1.0, stream=None) 
 
 
 def _once(kind, stream, x, *args, **kw):
-    """A prepared call made, run and dropped: what it allocates belongs to the
-    stream it runs on."""
+    """A prepared call made, run and dropped: what it allocates belongs to the stream
+    it runs on, and what it was given is not used again before that stream is done."""
     if not isinstance(x, torch.Tensor) or not x.is_cuda:
         raise DynconvError("a device tensor is needed")
     with torch.cuda.device(x.device):
         if stream is None:
             return kind(x, *args, **kw)()
         with torch.cuda.stream(stream):
-            return kind(x, *args, **kw)(stream)
+            call = kind(x, *args, **kw)
+            for t in call.keep:
+                if t is not None:
+                    t.record_stream(stream)
+            return call(stream)
 
 
 class GroupedLinear(_Prepared):

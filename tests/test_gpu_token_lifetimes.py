@@ -43,3 +43,50 @@ def test_prepared_calls_hold_their_tensors():
     del calls
     gc.collect()
     assert [name for name, r in held if r() is not None] == []
+
+
+def test_inputs_of_another_stream_are_not_given_away():
+    """A call on a side stream, its inputs dropped at once: their memory is not handed
+    out again before the side stream has read them."""
+    gen = torch.Generator(DEV).manual_seed(5)
+    logits = torch.randn((4096, 256), generator=gen, device=DEV)
+    x = torch.randn((2048, 64), generator=gen, device=DEV)
+    w = torch.randn((4, 32, 64), generator=gen, device=DEV)
+    starts = torch.tensor([0, 500, 900, 1500, 2048], dtype=torch.int32, device=DEV)
+    y = torch.zeros((2048, 32), device=DEV)
+    want = dc.route(logits, 4)
+    product = dc.grouped_linear(x, y, w, None, starts).clone()
+    side = torch.cuda.Stream()
+    y.zero_()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(200_000_000)  # the calls wait behind this
+    got = dc.route(logits, 4, stream=side)
+    dc.grouped_linear(x, y, w, None, starts, stream=side)
+    places = {t.data_ptr(): t.shape for t in (logits, x, w)}
+    del logits, x, w
+    for shape in list(places.values()) * 2:
+        again = torch.full(shape, 7.0, device=DEV)
+        assert again.data_ptr() not in places
+    torch.cuda.synchronize()
+    assert torch.equal(got.expert, want.expert) and torch.equal(got.weight, want.weight)
+    assert torch.equal(y, product)
+
+
+def test_one_shot_calls_in_a_graph():
+    """Captured on the stream they are given, replayed on new inputs."""
+    gen = torch.Generator(DEV).manual_seed(6)
+    logits = torch.randn((300, 24), generator=gen, device=DEV)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        got = dc.route(logits, 3, stream=side)
+    for i in range(4):
+        logits.copy_(torch.randn((300, 24), generator=gen, device=DEV))
+        graph.replay()
+        torch.cuda.synchronize()
+        want = dc.route(logits, 3)
+        torch.cuda.synchronize()
+        assert torch.equal(got.expert, want.expert) and torch.equal(got.weight, want.weight)
+        assert torch.equal(got.rows, want.rows) and torch.equal(got.starts, want.starts)
