@@ -66,3 +66,27 @@ def test_the_first_half_keeps_its_bits(dtype, rows, c_out):
     s["w"] = s["w"] * 0.125  # the adapters are what counts
     want, bound = expect(s, halves=True)
     within(call(s), want, bound, "first half")
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,c_out", FORMS)
+def test_ids_and_ranks_of_any_value(dtype, rows, c_out):
+    """Rows of all requests mixed, ids that name no adapter, ranks of nothing and past
+    the largest, an activation after the sum."""
+    s = case("any", rows, c_out, dtype, adapters=9)
+    s["ranks"][:5] = torch.tensor([0, 33, -4, 2 ** 31 - 1, 17], dtype=torch.int32)
+    s["ids"][1], s["ids"][3], s["ids"][rows - 1] = 9, -2 ** 31, 2 ** 31 - 1
+    want, bound = expect(s, dc.ACT_SILU)
+    within(call(s, dc.ACT_SILU), want, bound, "any order")
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,c_out", FORMS)
+def test_no_two_rows_of_a_request_together(dtype, rows, c_out):
+    """Every row another request's than the row before, more adapters than a workgroup
+    has rows in the small forms, ranks of 8 to 256."""
+    for max_rank in (8, 256 if rows < 1000 else 64):
+        s = case(("alternate", max_rank), rows, c_out, dtype, adapters=70, max_rank=max_rank)
+        s["ids"] = (torch.arange(rows) * 37 % 70).to(torch.int32)
+        want, bound = expect(s)
+        within(call(s), want, bound, "alternating rows")
