@@ -79,14 +79,14 @@ void launch_route_k(const void *logits, int64_t tokens, int E, int top_k, const 
     }
     int32_t *hist = at<int32_t>(ws, L.hist), *totals = at<int32_t>(ws, L.totals);
     const dim3 grid(static_cast<unsigned>(L.blocks));
-    // a row for each group of lanes at least; where there are more, more waves hide
-    // each other's waits
+    // a row for each group of lanes at least; where there are more (on whole waves
+    // always: 32 rows at least), more waves hide each other's waits
     auto choose = [&](auto kern, int threads) {
         launch(mk, kern, grid, dim3(threads), 0, st, static_cast<const T *>(logits), tokens, L.per, E, top_k, bias, mask,
                flags, scale, out->expert, out->weight, hist);
     };
-    if (L.per > kRouteThreads / G) choose(k_route_choose<T, G, V, 1024>, 1024);
-    else choose(k_route_choose<T, G, V, kRouteThreads>, kRouteThreads);
+    if (G == kWave || L.per > kRouteThreads / G) choose(k_route_choose<T, G, V, 1024>, 1024);
+    else if constexpr (G != kWave) choose(k_route_choose<T, G, V, kRouteThreads>, kRouteThreads);
     launch(mk, k_route_scan, dim3((E + kWavesPerBlock) / kWavesPerBlock), dim3(kBlock), 0, st, hist,
            static_cast<int>(L.blocks), E + 1, totals);
     launch(mk, k_route_lists, grid, dim3(kRouteThreads), sizeof(uint16_t) * kRouteWaves * (E + 1), st, out->expert,
