@@ -363,7 +363,8 @@ __device__ __forceinline__ void add_adapters(const RowsArgs &a, int row_id, int6
                             : none;
 #pragma unroll
             for (int b = 0; b < kOnce; ++b) {
-                u32x4 u = used_part<T>(uv[b], rank[b] - k);
+                u32x4 u = uv[b];
+                if (rank[b] % (16 / static_cast<int>(sizeof(T))) != 0) u = used_part<T>(u, rank[b] - k);
                 uint32_t odd = 0;
                 if (chunk_rest<T>(g)) u = finite_part<T>(u, odd);  // the first halves have brought the rest
 #pragma unroll
@@ -497,8 +498,9 @@ __device__ __forceinline__ void stream_products(const char *const (&rows)[2 * (N
 // Groups of a few rows: the time is that of reading the weights.  A workgroup
 // takes MF * 16 rows of a group and NF tiles of 16 weight rows (gated: the value's
 // and the gate's of 16 outputs); its NW waves split the contraction, stream it, and
-// add up through LDS in wave order.  80 KB of LDS leave two workgroups a CU, one's
-// loads under way while the other adds up.  64 tokens with 8 of 64 experts, 2048 ->
+// add up through LDS in wave order.  Up to 48 rows 80 KB of LDS leave two workgroups a
+// CU, one's loads under way while the other adds up; 64 rows take 96 KB, and adapters
+// 160 KB, for rings of two steps: one workgroup a CU.  64 tokens with 8 of 64 experts, 2048 ->
 // 2 x 1024 gated, bf16: 537 MB in 98 us, 5.5 TB/s (a large copy: 5.1); the projection
 // back, whose contraction is half as long, 268 MB in 65 us, 4.1 TB/s.  A step through
 // one 4096 x 4096 projection with 48 rows and 32 adapters of rank 16: 13.6 us, 2.8
@@ -671,16 +673,16 @@ k_rows_tile(RowsArgs a, int slices) {
         now.start(keys);
     }
     // Where the loads of step `step` come from; past the last step zeros.  The
-    // steps are taken in order.
+    // steps are taken in order.  own: a step of the rows' own contraction.
     const char *from[C::kLoads];
-    auto sources = [&](int step) {
+    auto sources = [&](int step, auto own) {
 #pragma unroll
         for (int i = 0; i < C::kLoads; ++i) {
             from[i] = left > 0 ? next[i] : zero;
             next[i] += 64;
         }
         left -= 64;
-        if constexpr (ADAPT) {
+        if constexpr (ADAPT && !decltype(own)::value) {
             if (step >= own_steps && step < steps) {
                 if (ahead.k0 >= ahead.rank) ahead.next(keys, my_rows);
                 const int k = ahead.k0 + chunk_rank<T>(lchunk);
@@ -711,8 +713,8 @@ k_rows_tile(RowsArgs a, int slices) {
         if constexpr (i < C::kLoadsX) load_to_lds<i * 1024>(from[i], xl + to);
         else load_to_lds<(i - C::kLoadsX) * 1024>(from[i], wl + to);
     };
-    auto load_all = [&](int step) {
-        sources(step);
+    auto load_all = [&](int step, auto own) {
+        sources(step, own);
         unrolled<C::kLoads>(load);
         to = after(to);
     };
@@ -738,7 +740,7 @@ k_rows_tile(RowsArgs a, int slices) {
 #pragma unroll
         for (int f = 0; f < MF; ++f) acc[i][f] = chunk_mma<T>(wv[i], xv[f], acc[i][f]);
     };
-    unrolled<C::kAhead>([&](auto step) { load_all(decltype(step)::value); });
+    unrolled<C::kAhead>([&](auto step) { load_all(decltype(step)::value, std::false_type()); });
     // where the wave's rows go: lane l has rows l, l + 64, .. of them
     constexpr int kTargets = (MF * 16 + kWave - 1) / kWave;
     int target[kTargets];
@@ -752,7 +754,7 @@ k_rows_tile(RowsArgs a, int slices) {
     if constexpr (C::kTwo) {
         loads_barrier<(C::kAhead - 1) * C::kLoads>();
         if (second) __builtin_amdgcn_s_barrier();
-        sources(C::kAhead);
+        sources(C::kAhead, std::false_type());
     }
     // A step of an adapter: its own rows' v, and zeros for the others.  Zeros would not
     // keep an infinity or NaN in up from the others, so those entries are taken out
@@ -769,7 +771,7 @@ k_rows_tile(RowsArgs a, int slices) {
         for (int i = 0; i < NF; ++i) wv[i] = finite_part<T>(wv[i], odd);
         unrolled<NF>(multiply);
     };
-    auto run = [&](int s0, int s1, auto products) {
+    auto run = [&](int s0, int s1, auto own, auto products) {
         for (int s = s0; s < s1; ++s) {
             if constexpr (C::kTwo) {
                 // Reading, and the loads of step s + kAhead, into the slot of step
@@ -782,7 +784,7 @@ k_rows_tile(RowsArgs a, int slices) {
                 loads_barrier<(C::kAhead - 1) * C::kLoads>();  // step s + 1 has landed
                 __builtin_amdgcn_sched_barrier(0);
                 __builtin_amdgcn_s_setprio(1);
-                sources(s + 1 + C::kAhead);
+                sources(s + 1 + C::kAhead, own);
                 products();
                 __builtin_amdgcn_s_setprio(0);
                 __builtin_amdgcn_sched_barrier(0);
@@ -790,15 +792,23 @@ k_rows_tile(RowsArgs a, int slices) {
                 __builtin_amdgcn_sched_barrier(0);
             } else {
                 loads_barrier<(C::kAhead - 1) * C::kLoads>();  // step s has landed, step s - 1 is read
-                load_all(s + C::kAhead);
+                load_all(s + C::kAhead, own);
                 read();
                 products();
             }
         }
     };
-    run(0, own_steps, [&]() { unrolled<NF>(multiply); });
-    if constexpr (ADAPT)
-        run(own_steps, steps, adapter_products);
+    auto own_products = [&]() { unrolled<NF>(multiply); };
+    if constexpr (ADAPT) {
+        // a loop without a choice of sources for as long as the loads are the rows' own
+        // (8192 rows of 8 adapters, 4096 x 4096: 250 us against 269 with a choice in each step)
+        const int plain = own_steps - (C::kTwo ? 1 : 0) - C::kAhead;
+        run(0, plain, std::true_type(), own_products);
+        run(plain < 0 ? 0 : plain, own_steps, std::false_type(), own_products);
+        run(own_steps, steps, std::false_type(), adapter_products);
+    } else {
+        run(0, steps, std::true_type(), own_products);
+    }
     if constexpr (C::kTwo)
         if (!second) __builtin_amdgcn_s_barrier();
     loads_barrier<0>();  // LDS is free: each wave takes its share for its sums
