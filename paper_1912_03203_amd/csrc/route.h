@@ -10,8 +10,9 @@
 // subtracted, or sigmoid; a bias never counts in them.
 //
 // Lists.  Assignment a = row * k + slot.  A counting sort that keeps the order:
-// the choosing workgroups count their assignments per expert, and the list
-// workgroups add up the counts of the workgroups before them.  Every rank comes
+// the choosing workgroups count their assignments per expert, k_route_scan adds up
+// the counts of the workgroups before each, and the list workgroups rank from there
+// (up to 128 rows one workgroup does all three).  Every rank comes
 // from ballots and sums of whole numbers, so the lists do not depend on timing.
 #pragma once
 

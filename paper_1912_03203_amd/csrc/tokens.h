@@ -122,7 +122,8 @@ struct RowsPlan {
 };
 
 // The form by the mean number of rows a group and the tiles that groups of that
-// size make (weight rows = outputs, twice as many when gated); bf16, us:
+// size make (weight rows = outputs, twice as many when gated); bf16, us, on groups of
+// equal size:
 //   few rows / 64-row tiles   32 groups 2048 -> 1024, 16 rows each 25.7 / 26.8, 32:
 //     28.3 / 28.4, 64: 47.6 / 34.1; 8 groups 1024 -> 2048, 32 rows 10.4 / 9.1.  Few
 //     rows up to 16, and beyond where the tiles would leave most CUs idle (a decoding
@@ -133,6 +134,13 @@ struct RowsPlan {
 //   128 / 256  one group of 2048 rows 2048 -> 4096 (128 tiles of 256) 46.2 / 48.7; 32
 //     groups of 256 rows 1024 -> 2048 (256 tiles) 59.9 / 48.2.  Likewise.  fp32 has no
 //     256-row tile: its products take 16 times as long, and fill the CUs with less.
+// On groups as a router makes them (choices of 2, the experts' logits spread by half
+// of the rows' own deviation) half of the groups pass a mean of 16 and take two tiles of
+// 16 rows, where the tiles of 64 still take one:
+//   few rows / 64-row tiles   32 groups 2048 -> 1024, mean 8 29.2 / 36.2, 16: 34.1 / 38.5,
+//     32: 40.0 / 39.5; 64 groups 1024 -> 2048, 8: 58.2 / 58.0, 16: 74.8 / 60.4; 8 groups 1024
+//     -> 2048, 16: 11.6 / 9.0: the rule is late for short contractions.
+//   128 / 256  32 groups of mean 256, 1024 -> 2048 70.6 / 72.6, of 512, 2048 -> 2048 208 / 186.
 RowsPlan rows_plan(int64_t rows, int64_t groups, bool adapt, int c_out, bool gated, dynconv_dtype dt) {
     RowsPlan p;
     const int64_t mean = (rows + groups - 1) / groups, used = std::min(rows, groups);
@@ -213,7 +221,12 @@ dynconv_status check_experts(const dynconv_experts *e, dynconv_dtype dt, int64_t
 }
 
 // Few tokens: one launch for the second product and the sum.  A token's experts
-// differ, so one token always gains; more do while their choices seldom meet.
+// differ, so one token always gains; more do while their choices seldom meet.  This
+// form multiplies one row a matrix instruction, so a second half of the hidden row is
+// free there.  Elsewhere it is not: with two halves the second product would read or
+// multiply twice the rows (an expert layer of long prompts a third more), so those
+// calls round h to the storage type, as this library's blocks do with their
+// intermediates, and a token's result is the more exact one in a call of few.
 bool few_tokens(int64_t tokens, int top_k, int experts) {
     return tokens == 1 || tokens * top_k * 2 <= experts;
 }
