@@ -581,7 +581,7 @@ dynconv_status dynconv_grouped_linear(const void *x, int64_t x_rows, void *y, in
  *   w_expand, w_gate [experts][c_hidden][c_in]; w_project [experts][c_out][c_hidden]
  * F_e(x) stays in fp32 until it is summed.  h is rounded to the storage type (fp16:
  * infinite past 65504), as the blocks' intermediates are; calls of one token, or of
- * so few that tokens * top_k * 2 <= experts, keep twice its bits, which costs nothing
+ * so few that tokens * top_k * 2 <= experts, keep twice its bits, which costs little
  * there: a row's result is closer to the formula in such a call than in a longer one.
  */
 typedef struct {

@@ -495,16 +495,16 @@ __device__ __forceinline__ void stream_products(const char *const (&rows)[2 * (N
 }
 
 // ------------------------------------------------------------- few rows
-// Groups of a few rows: the time is that of reading the weights.  A workgroup
-// takes MF * 16 rows of a group and NF tiles of 16 weight rows (gated: the value's
-// and the gate's of 16 outputs); its NW waves split the contraction, stream it, and
-// add up through LDS in wave order.  Up to 48 rows 80 KB of LDS leave two workgroups a
-// CU, one's loads under way while the other adds up; 64 rows take 96 KB, and adapters
-// 160 KB, for rings of two steps: one workgroup a CU.  64 tokens with 8 of 64 experts, 2048 ->
-// 2 x 1024 gated, bf16: 537 MB in 98 us, 5.5 TB/s (a large copy: 5.1); the projection
-// back, whose contraction is half as long, 268 MB in 65 us, 4.1 TB/s.  A step through
-// one 4096 x 4096 projection with 48 rows and 32 adapters of rank 16: 13.6 us, 2.8
-// TB/s, two thirds of it the chain of one workgroup a CU.
+// Groups of a few rows: the time is that of reading the weights.  A workgroup takes
+// MF * 16 rows of a group and NF tiles of 16 weight rows (gated: the value's and the
+// gate's of 16 outputs); its NW waves split the contraction, stream it, and add up
+// through LDS in wave order.  Up to 48 rows 80 KB of LDS leave two workgroups a CU,
+// one's loads under way while the other adds up; 64 rows take 96 KB, and adapters 128
+// to 160 KB: one workgroup a CU.  64 tokens with 8 of 64 experts, 2048 -> 2 x 1024
+// gated, bf16: 537 MB in 98 us, 5.5 TB/s (a large copy: 5.1); the projection back,
+// whose contraction is half as long, 268 MB in 65 us, 4.1 TB/s.  A step through one
+// 4096 x 4096 projection with 48 rows and 32 adapters of rank 16: 14.8 us, 2.5 TB/s,
+// two thirds of it the chain of one workgroup a CU.
 template <typename T, typename OT, int NW, int NF, int MF, bool GATED, bool ADAPT>
 __global__ void __launch_bounds__(NW * kWave)
 k_rows_few(RowsArgs a, int slices) {
@@ -594,7 +594,7 @@ k_rows_few(RowsArgs a, int slices) {
 // leave the overlap to the several workgroups of a CU: 64 x 64 for 777 rows 1024 ->
 // 2816, 16.2 us, bound by the chain of load, barrier and read of each step.  fp32
 // takes four 16x16x4 products where 16-bit types take one 16x16x32: 1499 rows of 12
-// groups, 264 -> 520, 10.1 us.
+// groups, 264 -> 520, 16.0 us.
 template <int BM, int BN>
 struct TileCfg {
     static constexpr int kWavesM = 2, kWavesN = BN >= 256 ? 4 : 2;
@@ -929,11 +929,12 @@ k_combine(const float *__restrict__ o, const int32_t *__restrict__ expert, const
 // the contraction each.  Slots and parts are added in their order, in fp32.
 //
 // Of the 16 rows of a matrix instruction one is needed.  In 16-bit types h comes as
-// two halves (its rounding, and what that left) on rows 0 and 8, so h keeps twice
-// the storage type's bits for some 0.5 us: the result's own rounding is what remains,
+// two halves (its rounding, and what that left) on rows 0 and 8, so h keeps twice the
+// storage type's bits for some 0.5 us: the result's own rounding is what remains,
 // where a rounded h adds an error as large (few outputs: 1.5 times the error).  One
-// token, 8 slots, 1024 -> 2048 bf16: 33.5 MB in 12.3 us against 13.5 for the grouped
-// product and the sum; two tokens with 8 of 64 experts, whole layer, 44.8 against 49.0.
+// token, 8 slots, 1024 -> 2048 bf16: 33.5 MB in 12.0 us, 2.8 TB/s, on 128 workgroups,
+// one for every other CU, against 13.5 for the grouped product and the sum; two
+// tokens with 8 of 64 experts, whole layer, 44.8 against 49.0.
 template <typename T, int NW>
 __global__ void __launch_bounds__(NW * kWave)
 k_project_tokens(const char *__restrict__ h, int64_t pitch, const int32_t *__restrict__ expert,
@@ -996,13 +997,14 @@ k_project_tokens(const char *__restrict__ h, int64_t pitch, const int32_t *__res
 
 // ------------------------------------------------ an adapter's first half
 // v[row] = scale * A_id x[row] as add_adapters takes it (16-bit types: in two
-// halves), for 16 rows a workgroup: one distinct adapter of the rows at a time, every gridDim.z-th from blockIdx.z, NF tiles of 16
-// of its rows.  The waves split the contraction, stream it, and add up through LDS
-// in wave order.  8192 rows of 4096 bf16, rank 32: 67 MB in 29 us, 2.3 TB/s (an
-// adapter's rows come from L2 for each 16 rows, four times as much); 32 rows a
-// workgroup were no faster (rank 16 45.1 against 41.4 us with the product after it,
-// rank 64 43.3 against 46.7).  48 rows with 32 adapters: 6.3 us, the chain of one
-// workgroup.
+// halves), for 16 rows a workgroup: one distinct adapter of the rows at a time, every
+// gridDim.z-th from blockIdx.z, NF tiles of 16 of its rows.  The waves split the
+// contraction, stream it, and add up through LDS in wave order.  8192 rows of 4096
+// bf16, rank 32: 67 MB in 29 us, 2.3 TB/s (an adapter's rows come from L2 for each 16
+// rows, four times as much); 32 rows a workgroup were no faster (rank 16 45.1 against
+// 41.4 us with the product after it, rank 64 43.3 against 46.7).  48 rows with 32
+// adapters: 6.7 us, the chain of one workgroup (48 workgroups, one for each adapter
+// that 16 rows can have: most CUs have none).
 constexpr int kDownWaves = 8;
 
 template <typename T, int NF>
